@@ -14,6 +14,9 @@
  *                           quantized, the new token enters the window
  *   skvq_decode_attention   one query token attends over packed + fp16 tokens
  *
+ * and, for many sequences of different lengths (further down), rotary positions (skvq_rope_apply) and the
+ * same cache in 4-bit pages: skvq_paged_append, skvq_paged_read, skvq_paged_attention.
+ *
  * Conventions
  *  - C99, plain pointers and sizes.  Pointers marked HOST are read during the
  *    call only.  Pointers marked DEVICE are HIP device memory that the caller
@@ -352,6 +355,200 @@ int skvq_read_yardstick(const void *src, size_t bytes, void *sink, void *hip_str
  * overlapping; write_bytes: a multiple of 4096, below 2^43; ratio: 1..8.  One workgroup of 256 threads per
  * 4 KB written, streaming loads and stores, on hip_stream, asynchronously. */
 int skvq_read_write_yardstick(const void *src, void *dst, size_t write_bytes, int32_t ratio, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Rotary positions.  A rotated head has the pairs of its first rotary_dim channels turned by
+ * position * frequency: (a, b) -> (a cos - b sin, b cos + a sin); the other channels stay.  Keys enter a
+ * cache rotated; queries are rotated at their own token's position.
+ *
+ * Numerics contract: the angle in turns is (position * F) mod 1 with the pair's F in 64-bit fixed point
+ * (exact but for F's own rounding, at any position); cosine and sine times the amplitude are rounded to
+ * fp32 once; the two products and their sum each round once in fp32 (no multiply-add), the result once
+ * to the tensor's type.  So rotated values are a pure function of the inputs, the same in every kernel. */
+typedef enum { SKVQ_DTYPE_F16 = 0, SKVQ_DTYPE_BF16 = 1, SKVQ_DTYPE_F32 = 2 } skvq_dtype;
+
+typedef enum {
+  SKVQ_ROPE_HALF = 0,       /* pair i: channels i and i + rotary_dim / 2 */
+  SKVQ_ROPE_INTERLEAVED = 1 /* pair i: channels 2i and 2i + 1            */
+} skvq_rope_layout;
+
+/* Frequencies f_i = base^(-2i / rotary_dim) (radians per token), scaled for contexts longer than trained on:
+ *   LINEAR  f_i / factor
+ *   NTK     base * factor^(rotary_dim / (rotary_dim - 2)) in base's place: the fastest pair stays, the
+ *           slowest is stretched by factor
+ *   YARN    (Peng et al., 2023) pairs of `high` and more turns over original_context keep f_i, those of
+ *           `low` and fewer get f_i / factor, a ramp over the pair index between them (its ends rounded
+ *           outwards to whole pairs, kept within 0 .. rotary_dim - 1); amplitude 0.1 ln(factor) + 1
+ *   BANDS   the same with the ramp over the turns themselves, t = original_context f_i / 2 pi:
+ *           (1 - s) f_i / factor + s f_i, s = clamp((t - low) / (high - low), 0, 1); amplitude 1 */
+typedef enum {
+  SKVQ_ROPE_SCALE_NONE = 0,
+  SKVQ_ROPE_SCALE_LINEAR = 1,
+  SKVQ_ROPE_SCALE_NTK = 2,
+  SKVQ_ROPE_SCALE_YARN = 3,
+  SKVQ_ROPE_SCALE_BANDS = 4
+} skvq_rope_scaling;
+
+#define SKVQ_ROPE_MAX_HEAD_DIM 256
+typedef struct {
+  int32_t head_dim;        /* 2 .. SKVQ_ROPE_MAX_HEAD_DIM                                            */
+  int32_t rotary_dim;      /* even, 2 .. head_dim: leading channels that are rotated                  */
+  int32_t layout;          /* skvq_rope_layout                                                       */
+  int32_t scaling;         /* skvq_rope_scaling                                                      */
+  double base;             /* > 0, e.g. 10000                                                        */
+  double factor;           /* > 0; read by every scaling but NONE; > 1 for YARN                      */
+  double original_context; /* > 0; read by YARN and BANDS                                            */
+  double low, high;        /* 0 < low < high; read by YARN and BANDS                                 */
+  double amplitude;        /* factor on cosine and sine; 0 selects the scaling's own                 */
+  const double *frequencies; /* HOST [rotary_dim / 2] or NULL: the caller's own, any finite radians per
+                              token; base and scaling are then not read (amplitude 0 is 1)            */
+} skvq_rope_config;
+
+typedef struct skvq_rope skvq_rope; /* opaque host object; holds no device memory, serves every device */
+
+int skvq_rope_create(const skvq_rope_config *cfg, skvq_rope **out);
+void skvq_rope_destroy(skvq_rope *rope); /* NULL is allowed */
+/* The frequencies in use: HOST out [rotary_dim / 2] and the amplitude; either may be NULL. */
+int skvq_rope_frequencies(const skvq_rope *rope, double *frequencies, double *amplitude);
+
+/* One tensor of [batch][tokens][heads][head_dim] in any order: element strides, channels contiguous.
+ * y may be x with the same strides (in place); other overlaps give unspecified values. */
+typedef struct {
+  const void *x; /* DEVICE */
+  void *y;       /* DEVICE */
+  int64_t x_batch, x_token, x_head;
+  int64_t y_batch, y_token, y_head;
+  int32_t n_heads;
+} skvq_rope_tensor;
+
+/* Rotates one or two tensors (queries and keys, whose heads may differ in number) of one type in one launch.
+ * positions: DEVICE int32 [batch][tokens] with positions_batch elements between sequences (0: one row for
+ * all), or NULL: token t is at position start + t.  Positions may be negative; start and start + n_tokens
+ * must lie within 32 bits.  transpose != 0 turns by minus the angle, amplitude as it is: the gradient of the
+ * forward call, y the gradient of x.  16-byte accesses are used where base, strides, rotary_dim and head_dim
+ * allow them, else one channel at a time.  batch, n_tokens or n_heads of 0: nothing is done. */
+int skvq_rope_apply(const skvq_rope *rope, const skvq_rope_tensor *tensors, int32_t n_tensors, int32_t dtype,
+                    int32_t batch, int64_t n_tokens, const int32_t *positions, int64_t positions_batch,
+                    int64_t start, int32_t transpose, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The paged cache: many sequences of different lengths in one pool of pages, 4-bit keys and values.
+ * The quantizer (reorder, groups, clip scales, Eq. 2), the fp16 window and the sinks are those of
+ * skvq_cache; what differs is where a token lives and that lengths are device data:
+ *
+ *  - Token a of a sequence of T cached tokens: the last min(T, W) tokens are in the sequence's slot of
+ *    k_rows / v_rows, token a in row a % W; of the older ones token a < S is row W + a there, and token
+ *    a >= S is packed row te = a - S, in page page_table[te / P] of the sequence at place te % P.
+ *  - A page holds P packed rows of every kv head, Hk parts one after the other, each of four sections:
+ *      key codes    P x 64 bytes.  Reordered position p = 32 j + 8 g + e of a row is nibble e/2 (e even) or
+ *                   4 + e/2 (e odd) of the row's dword 4 g + j
+ *      value codes  P/4 x 256 bytes: four rows together.  Position p = 16 n + m of row r of the four is in
+ *                   bytes 16 m .. 16 m + 15, byte 8 (r/2) + 4 (n/4) + 2 (r%2) + (n%4)/2, low nibble if n even
+ *      key pairs    P x D/G (scale, zero) pairs in meta_format; then value pairs likewise
+ *    A page moves as one run of bytes, and its rows mean the same in any other place or pool of the format.
+ *  - A batch names the sequences of a call, their lengths, page tables and new tokens in device memory.
+ *    Nothing of it is read on the host, so calls may be captured into a graph and replayed with the
+ *    arrays' contents changed in between (stream order).  Nothing is allocated by a call.
+ *  - Device data is checked where it is used: an entry that would lead out of the buffers is not followed,
+ *    the sequence is left out (nothing of it is written; a page that cannot be followed leaves its rows out
+ *    of an append or a read; attention over it gives NaN), and the cache's error bits say so
+ *    (skvq_paged_errors).
+ *  - Two sequences may share pages that neither writes (a common prefix).  A slot or a page written by two
+ *    sequences of one call holds unspecified values of theirs afterwards.
+ *  - Calls on one cache must not overlap (one stream, or ordered streams); two graphs of one cache neither. */
+typedef struct skvq_paged skvq_paged; /* opaque host object */
+
+typedef struct {
+  int32_t n_q_heads;   /* Hq, a multiple of n_kv_heads with Hq/Hk <= 16                               */
+  int32_t n_kv_heads;  /* Hk                                                                          */
+  int32_t head_dim;    /* D, must be 128                                                              */
+  int32_t group_size;  /* G in {32, 64, 128}                                                          */
+  int32_t k_bits, v_bits; /* SKVQ_BITS_4 each                                                         */
+  int32_t window;      /* W >= 1                                                                      */
+  int32_t n_sink;      /* S >= 0                                                                      */
+  int32_t meta_format; /* skvq_meta_format                                                            */
+  int32_t dtype;       /* skvq_dtype of keys, values, queries, rows and outputs: F16 or BF16.  BF16
+                          inputs beyond fp16's range want SKVQ_META_F32                               */
+  int32_t page_size;   /* P in {16, 32, 64, 128, 256}                                                 */
+  int32_t n_pages;     /* pages of the pool                                                           */
+  int32_t max_seqs;    /* slots of k_rows / v_rows; most sequences of a batch                         */
+  int32_t max_tokens;  /* most query tokens of an attention call, all sequences together              */
+  const int32_t *perm_k, *perm_v; /* HOST, as in skvq_config                                          */
+  const float *clip_k, *clip_v;   /* HOST, as in skvq_config                                          */
+  float sm_scale;      /* softmax scale; 0 selects 1/sqrt(D)                                          */
+} skvq_paged_config;
+
+/* DEVICE buffers, 16-byte aligned; byte sizes from skvq_paged_sizes, in this order.
+ *   pages      u8   [n_pages][Hk][P * (128 + 4 * D/G * size of a meta value)]
+ *   k_rows     f16 or bf16 [max_seqs][Hk][W + S][D]
+ *   v_rows     likewise
+ *   workspace  partials of an attention call; scratch, any content is fine before a call */
+typedef struct {
+  void *pages, *k_rows, *v_rows, *workspace;
+} skvq_paged_buffers;
+
+int skvq_paged_sizes(const skvq_paged_config *cfg, size_t bytes[4]);
+int skvq_paged_validate_config(const skvq_paged_config *cfg);
+/* As skvq_create: copies the constants to the current device (synchronously), borrows the buffers. */
+int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bufs, skvq_paged **out);
+void skvq_paged_destroy(skvq_paged *cache); /* NULL is allowed */
+
+/* The sequences of a call.  Sequence i's new tokens (for skvq_paged_read: its tokens to read) are rows
+ * cu_tokens[i] .. cu_tokens[i+1]-1 of the call's token arrays; it has seq_lens[i] tokens cached once its new
+ * ones are in (the same arrays serve skvq_paged_append and the skvq_paged_attention after it).  A sequence
+ * may have no tokens in a call.  Rows at and beyond cu_tokens[n_seqs] are left as they were. */
+typedef struct {
+  int32_t n_seqs;            /* 0 .. max_seqs                                                            */
+  int32_t n_tokens;          /* rows of the token arrays (at most this many are read or written)          */
+  const int32_t *cu_tokens;  /* DEVICE [n_seqs + 1], ascending from 0                                     */
+  const int32_t *seq_lens;   /* DEVICE [n_seqs]                                                           */
+  const int32_t *page_table; /* DEVICE [n_seqs][table_stride]; entries of unused pages are not read        */
+  int32_t table_stride;      /* >= 1                                                                      */
+  const int32_t *slots;      /* DEVICE [n_seqs]: row slot of each sequence, or NULL: sequence i has slot i */
+  const int32_t *positions;  /* DEVICE [n_tokens]: rotary position of each new token, or NULL: its number
+                                in the sequence (skvq_paged_append only)                                  */
+  const int32_t *first;      /* DEVICE [n_seqs] or NULL: first token to read (skvq_paged_read only); NULL:
+                                the last ones                                                             */
+} skvq_batch;
+
+/* Section 3.2 for a batch: sequence i gains its new tokens.  Each key is rotated (rope; NULL: stored as it
+ * comes), every token that no longer is one of the last W goes to its sink row or is quantized into its packed
+ * row (Eq. 2 as at skvq_prefill_quantize, from the value rounded to the cache's type), the others enter the
+ * window.  Any number of new tokens per sequence: a decode step, a chunk of a prompt, a whole prompt.
+ * k, v: DEVICE [n_tokens][Hk][D] in the cache's type, k_stride / v_stride elements between tokens (so the rows
+ * of one fused projection serve as they are).  q: DEVICE [n_tokens][Hq][D] or NULL: rotated likewise (copied
+ * without rope) into q_out, which may be q with the same stride.  Bases 16-byte aligned, strides multiples
+ * of 8 elements and at least a row.  The cache's pages of a sequence must be in its page table beforehand. */
+int skvq_paged_append(skvq_paged *cache, const skvq_rope *rope, const skvq_batch *batch, const void *k,
+                      int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                      void *q_out, int64_t q_out_stride, void *hip_stream);
+
+/* Cached tokens as rows: token first[i] + j (NULL: seq_lens[i] - n_i + j) of sequence i, dequantized
+ * (scale * code, + zero, each rounded to fp32, then to the cache's type) or copied, in original channel
+ * order, keys rotated as they are stored.  k, v: DEVICE [n_tokens][Hk][D], strides as above.  Either may
+ * be NULL. */
+int skvq_paged_read(skvq_paged *cache, const skvq_batch *batch, void *k, int64_t k_stride, void *v,
+                    int64_t v_stride, void *hip_stream);
+
+/* Eq. 1 for the batch's query tokens, each over the tokens of its sequence up to and including itself, in the
+ * form they are stored in now: query j of n_i new tokens sees tokens 0 .. seq_lens[i] - n_i + j.
+ * q: DEVICE [n_tokens][Hq][D], rotated as the keys are; out: likewise, in the cache's type, or NULL; out_f32: DEVICE
+ * fp32 [n_tokens][Hq][D] contiguous, or NULL (not both).  Scores and sums in fp32; softmax weights enter the
+ * value product as fp16 numbers (half a step of 2^-11 each; bf16 rows as two bf16 parts).
+ * SKVQ_ERR_INVALID_ARG if n_tokens > max_tokens. */
+int skvq_paged_attention(skvq_paged *cache, const skvq_batch *batch, const void *q, int64_t q_stride, void *out,
+                         int64_t out_stride, float *out_f32, void *hip_stream);
+
+/* What the device checks have found since the last call: OR of these bits, then cleared.  Waits for the
+ * stream. */
+#define SKVQ_PAGED_BAD_COUNTS 1 /* cu_tokens not ascending within [0, n_tokens], or more new tokens than seq_lens */
+#define SKVQ_PAGED_BAD_SLOT 2   /* a slot outside [0, max_seqs)                                            */
+#define SKVQ_PAGED_BAD_PAGE 4   /* a needed page table entry outside [0, n_pages), or beyond table_stride   */
+#define SKVQ_PAGED_BAD_RANGE 8  /* first outside the sequence's tokens                                     */
+int skvq_paged_errors(skvq_paged *cache, int32_t *bits, void *hip_stream);
+
+/* The cache's last HIP error text (owned by cache). */
+const char *skvq_paged_last_error(const skvq_paged *cache);
 
 /* Static description of a status code; the cache's last HIP error text (owned by cache). */
 const char *skvq_status_string(int status);

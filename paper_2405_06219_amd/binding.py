@@ -22,6 +22,11 @@ SKVQ_MAX_SPLITS = 128
 SKVQ_STATIC_MAX_ROWS = 64
 HEAD_DIM = 128
 BUFFER_NAMES = ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win", "workspace")
+PAGED_BUFFER_NAMES = ("pages", "k_rows", "v_rows", "workspace")
+SKVQ_PAGED_BAD_COUNTS, SKVQ_PAGED_BAD_SLOT, SKVQ_PAGED_BAD_PAGE, SKVQ_PAGED_BAD_RANGE = 1, 2, 4, 8
+DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}   # skvq_dtype
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 
 class skvq_config(C.Structure):
@@ -36,6 +41,34 @@ class skvq_config(C.Structure):
 
 class skvq_buffers(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in BUFFER_NAMES]
+
+
+class skvq_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("original_context", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("amplitude", C.c_double), ("frequencies", C.c_void_p)]
+
+
+class skvq_rope_tensor(C.Structure):
+    _fields_ = ([("x", C.c_void_p), ("y", C.c_void_p)]
+                + [(n, C.c_int64) for n in ("x_batch", "x_token", "x_head", "y_batch", "y_token", "y_head")]
+                + [("n_heads", C.c_int32)])
+
+
+class skvq_paged_config(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "group_size", "k_bits", "v_bits", "window",
+                                          "n_sink", "meta_format", "dtype", "page_size", "n_pages", "max_seqs", "max_tokens")]
+                + [(n, C.c_void_p) for n in ("perm_k", "perm_v", "clip_k", "clip_v")] + [("sm_scale", C.c_float)])
+
+
+class skvq_paged_buffers(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in PAGED_BUFFER_NAMES]
+
+
+class skvq_batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("cu_tokens", C.c_void_p), ("seq_lens", C.c_void_p),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int32), ("slots", C.c_void_p), ("positions", C.c_void_p),
+                ("first", C.c_void_p)]
 
 
 _lib = None
@@ -79,6 +112,25 @@ def lib() -> C.CDLL:
         L.skvq_set_num_splits.argtypes = [C.c_void_p, C.c_int32]
         L.skvq_read_yardstick.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.skvq_read_write_yardstick.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p]
+        L.skvq_rope_create.argtypes = [C.POINTER(skvq_rope_config), C.POINTER(C.c_void_p)]
+        L.skvq_rope_destroy.argtypes = [C.c_void_p]
+        L.skvq_rope_destroy.restype = None
+        L.skvq_rope_frequencies.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+        L.skvq_rope_apply.argtypes = [C.c_void_p, C.POINTER(skvq_rope_tensor), C.c_int32, C.c_int32, C.c_int32, C.c_int64,
+                                      C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p]
+        L.skvq_paged_sizes.argtypes = [C.POINTER(skvq_paged_config), C.POINTER(C.c_size_t)]
+        L.skvq_paged_validate_config.argtypes = [C.POINTER(skvq_paged_config)]
+        L.skvq_paged_create.argtypes = [C.POINTER(skvq_paged_config), C.POINTER(skvq_paged_buffers), C.POINTER(C.c_void_p)]
+        L.skvq_paged_destroy.argtypes = [C.c_void_p]
+        L.skvq_paged_destroy.restype = None
+        L.skvq_paged_append.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p,
+                                        C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.skvq_paged_read.argtypes = [C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.skvq_paged_attention.argtypes = [C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                           C.c_void_p, C.c_void_p]
+        L.skvq_paged_errors.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]
+        L.skvq_paged_last_error.argtypes = [C.c_void_p]
+        L.skvq_paged_last_error.restype = C.c_char_p
         L.skvq_status_string.argtypes = [C.c_int]
         L.skvq_status_string.restype = C.c_char_p
         L.skvq_last_error.argtypes = [C.c_void_p]
@@ -402,3 +454,247 @@ class SkvqCache:
                 raw["v_meta"].view(META_DTYPES[self.cfg.meta_format]).reshape(b, hk, tcap, ng, 2),
                 raw["k_win"].view(np.uint16).reshape(b, hk, self.cfg.window + self.cfg.n_sink, HEAD_DIM),
                 raw["v_win"].view(np.uint16).reshape(b, hk, self.cfg.window + self.cfg.n_sink, HEAD_DIM)]
+
+
+# ---- rotary positions and the paged cache ------------------------------------------------------------------
+
+
+def _stream_on(device: torch.device, stream) -> int:
+    """The stream's handle; without one, the current stream of the tensors' device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index or 0)
+    return int(stream.cuda_stream)
+
+
+class SkvqRope:
+    """Rotary positions: frequencies of the first rotary_dim channels of a head, as skvq_rope_config takes them."""
+
+    def __init__(self, head_dim=HEAD_DIM, rotary_dim=None, layout="half", base=10000.0, scaling="none", factor=0.0,
+                 original_context=0.0, low=0.0, high=0.0, amplitude=0.0, frequencies=None):
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        own = None
+        if frequencies is not None:
+            own = np.ascontiguousarray(frequencies, np.float64)
+            if own.shape != (rotary_dim // 2,):
+                raise ValueError("frequencies needs rotary_dim / 2 entries")
+        cfg = skvq_rope_config(head_dim, rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], base, factor,
+                               original_context, low, high, amplitude, own.ctypes.data if own is not None else None)
+        handle = C.c_void_p()
+        rc = lib().skvq_rope_create(C.byref(cfg), C.byref(handle))
+        if rc != SKVQ_OK:
+            raise SkvqError(rc)
+        self._h, self.head_dim, self.rotary_dim = handle, head_dim, rotary_dim
+
+    def __del__(self):
+        try:
+            if getattr(self, "_h", None):
+                lib().skvq_rope_destroy(self._h)
+                self._h = None
+        except Exception:
+            pass
+
+    def skvq_rope_frequencies(self):
+        """(radians per token of every pair, amplitude)."""
+        f, a = np.zeros(self.rotary_dim // 2, np.float64), C.c_double()
+        rc = lib().skvq_rope_frequencies(self._h, f.ctypes.data, C.addressof(a))
+        if rc != SKVQ_OK:
+            raise SkvqError(rc)
+        return f, a.value
+
+    def skvq_rope_apply(self, q: torch.Tensor, k: torch.Tensor | None = None, positions: torch.Tensor | None = None, start=0,
+                        out_q: torch.Tensor | None = None, out_k: torch.Tensor | None = None, transpose=False, stream=None):
+        """q, k [B][T][heads][head_dim] with any strides but the last dimension's; positions int32 [T] or [B][T], or
+        None: start + t.  transpose: the gradient's way back.  Returns q's result, or (q's, k's); out_q / out_k may
+        be q / k (in place)."""
+        xs, outs = ([q], [out_q]) if k is None else ([q, k], [out_q, out_k])
+        if q.dtype not in DTYPES:
+            raise ValueError(f"rotary positions take fp16, bf16 and fp32 tensors, got {q.dtype}")
+        b, t = q.shape[:2]
+        tensors = (skvq_rope_tensor * len(xs))()
+        for i, x in enumerate(xs):
+            if outs[i] is None:
+                outs[i] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            for y in (x, outs[i]):
+                if not (y.is_cuda and y.device == q.device and y.dtype == q.dtype and y.dim() == 4 and y.shape[:2] == (b, t)
+                        and y.shape == x.shape and y.shape[3] == self.head_dim and (y.stride(3) == 1 or y.numel() == 0)):
+                    raise ValueError(f"expected {q.dtype} tensors [{b}][{t}][heads][{self.head_dim}] on {q.device}, channels "
+                                     f"contiguous, got {y.dtype} {tuple(y.shape)} on {y.device}, strides {y.stride()}")
+            tensors[i] = skvq_rope_tensor(x.data_ptr(), outs[i].data_ptr(), *x.stride()[:3], *outs[i].stride()[:3], x.shape[2])
+        at, stride = None, 0
+        if positions is not None:
+            if positions.dtype != torch.int32 or positions.device != q.device or positions.shape not in ((t,), (b, t)) or (
+                    t > 1 and positions.stride(-1) != 1):
+                raise ValueError(f"positions must be int32 [{t}] or [{b}][{t}] on {q.device}")
+            at, stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
+        call = (self._h, tensors, len(xs), DTYPES[q.dtype], b, t, at, stride, start, int(transpose), _stream_on(q.device, stream))
+        if q.device.index == torch._C._cuda_getDevice():
+            rc = lib().skvq_rope_apply(*call)
+        else:
+            with torch.cuda.device(q.device):
+                rc = lib().skvq_rope_apply(*call)
+        if rc != SKVQ_OK:
+            raise SkvqError(rc)
+        return outs[0] if k is None else (outs[0], outs[1])
+
+
+class SkvqBatch:
+    """The sequences of a call (skvq_batch): int32 tensors on the cache's device, read when a call runs, so their contents
+    may change between calls.  n_tokens: rows of the token tensors; None reads cu_tokens' last entry (and waits)."""
+
+    def __init__(self, cu_tokens: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor, slots=None, positions=None,
+                 first=None, n_tokens=None):
+        n = seq_lens.shape[0]
+        if n_tokens is None:
+            n_tokens = int(cu_tokens[-1])
+        if page_table.dim() != 2 or page_table.shape[0] != n:
+            raise ValueError("page_table must be [n_seqs][pages]")
+        shapes = {"cu_tokens": (cu_tokens, (n + 1,)), "seq_lens": (seq_lens, (n,)), "page_table": (page_table, tuple(page_table.shape)),
+                  "slots": (slots, (n,)), "positions": (positions, (n_tokens,)), "first": (first, (n,))}
+        for name, (t, shape) in shapes.items():
+            if t is not None and not (t.dtype == torch.int32 and t.is_cuda and t.device == seq_lens.device and t.is_contiguous()
+                                      and tuple(t.shape) == shape):
+                raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {seq_lens.device}")
+        self.tensors = [t for t, _ in shapes.values()]   # kept alive
+        self.device, self.n_seqs, self.n_tokens = seq_lens.device, n, n_tokens
+
+        def ptr(t):
+            return t.data_ptr() if t is not None else None
+
+        self.struct = skvq_batch(n, n_tokens, ptr(cu_tokens), ptr(seq_lens), ptr(page_table), page_table.shape[1], ptr(slots),
+                                 ptr(positions), ptr(first))
+
+
+def make_paged_config(n_q_heads, n_kv_heads, group_size, window, page_size, n_pages, max_seqs, max_tokens, perm_k, perm_v,
+                      clip_k, clip_v, sm_scale=0.0, k_bits=4.0, v_bits=4.0, head_dim=HEAD_DIM, n_sink=0, meta="f16",
+                      dtype=torch.float16):
+    """Returns (skvq_paged_config, keepalive): the numpy arrays the config points to."""
+    keep = [np.ascontiguousarray(perm_k, np.int32), np.ascontiguousarray(perm_v, np.int32),
+            np.ascontiguousarray(clip_k, np.float32), np.ascontiguousarray(clip_v, np.float32)]
+    shapes = [(n_kv_heads, head_dim)] * 2 + [(n_kv_heads, head_dim // max(group_size, 1))] * 2
+    if [a.shape for a in keep] != shapes:
+        raise ValueError("perm must be [n_kv_heads][head_dim], clip [n_kv_heads][head_dim / group_size]")
+    cfg = skvq_paged_config(n_q_heads, n_kv_heads, head_dim, group_size, bits_enum(k_bits), bits_enum(v_bits), window, n_sink,
+                            META_FORMATS[meta], DTYPES[dtype], page_size, n_pages, max_seqs, max_tokens,
+                            *[a.ctypes.data for a in keep], float(sm_scale))
+    return cfg, keep
+
+
+def skvq_paged_sizes(cfg: skvq_paged_config) -> list[int]:
+    out = (C.c_size_t * 4)()
+    rc = lib().skvq_paged_sizes(C.byref(cfg), out)
+    if rc != SKVQ_OK:
+        raise SkvqError(rc)
+    return [int(x) for x in out]
+
+
+def skvq_paged_validate_config(cfg: skvq_paged_config) -> int:
+    return int(lib().skvq_paged_validate_config(C.byref(cfg)))
+
+
+class SkvqPagedCache:
+    """One layer's paged cache: owns the library handle and the device buffers (or adopts those of `buffers`, a dict of
+    tensors under the names of skvq_paged_buffers; the others are allocated)."""
+
+    def __init__(self, n_q_heads, n_kv_heads, group_size, window, page_size, n_pages, max_seqs, max_tokens, perm_k, perm_v,
+                 clip_k, clip_v, sm_scale=0.0, k_bits=4.0, v_bits=4.0, n_sink=0, meta="f16", dtype=torch.float16,
+                 device="cuda:0", buffers=None):
+        self.cfg, self._keep = make_paged_config(n_q_heads, n_kv_heads, group_size, window, page_size, n_pages, max_seqs,
+                                                 max_tokens, perm_k, perm_v, clip_k, clip_v, sm_scale, k_bits, v_bits,
+                                                 n_sink=n_sink, meta=meta, dtype=dtype)
+        self.heads, self.dtype = (n_q_heads, n_kv_heads), dtype
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.sizes = skvq_paged_sizes(self.cfg)
+        self.buffers = {}
+        for name, nbytes in zip(PAGED_BUFFER_NAMES, self.sizes):
+            t = (buffers or {}).get(name)
+            if t is None:
+                t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            elif t.device != self.device or not t.is_contiguous() or t.numel() * t.element_size() != nbytes:
+                raise ValueError(f"buffer {name} must be a contiguous tensor of {nbytes} bytes on {self.device}")
+            self.buffers[name] = t
+        bufs = skvq_paged_buffers(*[self.buffers[n].data_ptr() for n in PAGED_BUFFER_NAMES])
+        handle = C.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = lib().skvq_paged_create(C.byref(self.cfg), C.byref(bufs), C.byref(handle))
+        if rc != SKVQ_OK:
+            raise SkvqError(rc)
+        self._h = handle
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().skvq_paged_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc):
+        if rc != SKVQ_OK:
+            raise SkvqError(rc, lib().skvq_paged_last_error(self._h).decode())
+
+    def _rows(self, t: torch.Tensor, n: int, heads: int) -> tuple[int, int]:
+        """(address, elements between tokens) of rows [n][heads][D] whose heads lie one after the other."""
+        if not (t.dtype == self.dtype and t.device == self.device and t.shape == (n, heads, HEAD_DIM)
+                and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == HEAD_DIM)))):
+            raise ValueError(f"expected {self.dtype} rows [{n}][{heads}][{HEAD_DIM}] on {self.device}, heads contiguous, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+        # (the stride of a dimension of one token says nothing)
+        return t.data_ptr(), t.stride(0) if n > 1 else heads * HEAD_DIM
+
+    def _batch(self, batch: SkvqBatch):
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
+        return C.byref(batch.struct), batch.n_tokens
+
+    def _new(self, n: int, heads: int, dtype=None):
+        return torch.empty((n, heads, HEAD_DIM), dtype=dtype or self.dtype, device=self.device)
+
+    def skvq_paged_append(self, batch: SkvqBatch, k: torch.Tensor, v: torch.Tensor, rope: SkvqRope | None = None,
+                          q: torch.Tensor | None = None, out_q: torch.Tensor | None = None, stream=None):
+        """k, v [n_tokens][Hk][D]: the batch's new tokens.  With q [n_tokens][Hq][D] returns its rotated rows (in out_q,
+        which may be q)."""
+        bp, n = self._batch(batch)
+        kp, vp = self._rows(k, n, self.heads[1]), self._rows(v, n, self.heads[1])
+        qp = op = (None, 0)
+        if q is not None:
+            qp = self._rows(q, n, self.heads[0])
+            out_q = self._new(n, self.heads[0]) if out_q is None else out_q
+            op = self._rows(out_q, n, self.heads[0])
+        self._check(lib().skvq_paged_append(self._h, rope._h if rope is not None else None, bp, *kp, *vp, *qp, *op,
+                                            _stream_on(self.device, stream)))
+        return out_q
+
+    def skvq_paged_read(self, batch: SkvqBatch, out_k: torch.Tensor | None = None, out_v: torch.Tensor | None = None,
+                        stream=None):
+        """Cached tokens back as (k, v) [n_tokens][Hk][D]: batch.first's, or each sequence's last ones."""
+        bp, n = self._batch(batch)
+        out_k = self._new(n, self.heads[1]) if out_k is None else out_k
+        out_v = self._new(n, self.heads[1]) if out_v is None else out_v
+        self._check(lib().skvq_paged_read(self._h, bp, *self._rows(out_k, n, self.heads[1]), *self._rows(out_v, n, self.heads[1]),
+                                          _stream_on(self.device, stream)))
+        return out_k, out_v
+
+    def skvq_paged_attention(self, batch: SkvqBatch, q: torch.Tensor, out: torch.Tensor | None = None,
+                             out_f32: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """q [n_tokens][Hq][D]: returns out (allocated unless given; not written where only out_f32 is given)."""
+        bp, n = self._batch(batch)
+        qp = self._rows(q, n, self.heads[0])
+        if out is None and out_f32 is None:
+            out = self._new(n, self.heads[0])
+        op = self._rows(out, n, self.heads[0]) if out is not None else (None, 0)
+        fp = None
+        if out_f32 is not None:
+            fp = _dev_ptr(out_f32, torch.float32, (n, self.heads[0], HEAD_DIM))
+        self._check(lib().skvq_paged_attention(self._h, bp, *qp, *op, fp, _stream_on(self.device, stream)))
+        return out if out is not None else out_f32
+
+    def skvq_paged_errors(self, stream=None) -> int:
+        """Error bits (SKVQ_PAGED_BAD_*) that the device checks have set since the last call; waits for the stream."""
+        bits = C.c_int32()
+        self._check(lib().skvq_paged_errors(self._h, C.byref(bits), _stream_on(self.device, stream)))
+        return bits.value

@@ -1,0 +1,109 @@
+// How the paged cache's kernels deal a batch out: which workgroup has which rows of which sequence, and where a row
+// goes.  Plain constexpr arithmetic without device types, so that the host can check it at every length.
+#pragma once
+
+namespace skvq {
+
+// Workgroups are dealt to sequences without a prefix sum: sequence i, whose new tokens begin at row0, has the units from
+// unit_start(row0, i) on, and at most n_new * mul / 2^div_log2 + pad (rounded down) of them, for which the next
+// sequence's start leaves room: floor(x + y) >= floor(x) + floor(y).
+struct UnitDeal {
+  int mul, div_log2, pad;
+};
+constexpr UnitDeal kAppendDeal{1, 2, 3};
+constexpr UnitDeal kReadDeal{1, 2, 2};
+constexpr UnitDeal kTokenDeal{1, 0, 0};
+constexpr UnitDeal row_deal(int query_heads) { return UnitDeal{query_heads, 4, 1}; }  // blocks of 16 query rows
+constexpr long long unit_start(const UnitDeal &d, int row0, int i) {
+  return (((long long)row0 * d.mul) >> d.div_log2) + (long long)i * d.pad;
+}
+
+// Token a is packed row a - S.  Kernels take packed rows by fours (they share their value codes' bytes, and lie in one
+// page, whose size is a multiple of 16): tokens with the same (a + lead) / 4.
+constexpr int lead_of(int S) { return (4 - (S & 3)) & 3; }
+
+// Append, with `len` tokens cached before and `total` after: the tokens that leave the window are [lo, hi) =
+// [max(0, len - W), total - W): ring rows and, of a long prompt, new tokens that never were in the ring.  A ring row is
+// overwritten by the lanes that have read it: those that pack old token a also write its successor, the newest token
+// of the same row.  Rows that held nothing (len < W) are fours of their own.
+struct AppendPlan {
+  int W, S, total, len, lo, hi, lead, four0, leaving_fours, vacant_end, vacant_fours;
+};
+constexpr AppendPlan append_plan(int total, int n_new, int W, int S) {
+  AppendPlan p{W, S, total, total - n_new, 0, 0, lead_of(S), 0, 0, 0, 0};
+  p.lo = p.len > W ? p.len - W : 0;
+  p.hi = total - W > p.lo ? total - W : p.lo;
+  p.four0 = (p.lo + p.lead) >> 2;
+  p.leaving_fours = p.hi > p.lo ? ((p.hi + p.lead + 3) >> 2) - p.four0 : 0;
+  p.vacant_end = total < W ? total : W;
+  p.vacant_fours = p.len < p.vacant_end ? (p.vacant_end - p.len + 3) >> 2 : 0;
+  return p;
+}
+struct AppendRow {
+  bool valid;    // there is something to do
+  bool leaving;  // token `token` leaves: to its sink row (sink) or packed row te
+  bool old;      // ... from ring row `ring`
+  bool sink;
+  int token, te;
+  int fresh;     // the new token to load: the leaving one itself, or what enters ring row `ring` (-1: none)
+  int ring;
+};
+constexpr AppendRow append_row(const AppendPlan &p, int unit, int r) {
+  AppendRow x{false, unit < p.leaving_fours, false, false, -1, -1, 0, -1};
+  if (x.leaving) {
+    const int a = 4 * (p.four0 + unit) + r - p.lead;
+    x.valid = a >= p.lo && a < p.hi;
+    x.token = a;
+    x.old = a < p.len;
+    x.sink = a < p.S;
+    x.te = a - p.S;
+    x.fresh = x.old ? a + (p.total - 1 - a) / p.W * p.W : a;
+    if (x.old) x.ring = a % p.W;
+  } else {
+    x.ring = p.len + 4 * (unit - p.leaving_fours) + r;
+    x.valid = x.ring < p.vacant_end;
+    x.fresh = x.ring + (p.total - 1 - x.ring) / p.W * p.W;
+  }
+  return x;
+}
+
+// Read of tokens [first, first + n): fours, and where a token is.
+constexpr int read_fours(int first, int n, int S) { return n > 0 ? ((first + n + lead_of(S) + 3) >> 2) - ((first + lead_of(S)) >> 2) : 0; }
+constexpr int read_token(int first, int S, int unit, int r) { return 4 * (((first + lead_of(S)) >> 2) + unit) + r - lead_of(S); }
+struct TokenPlace {
+  bool full;  // in a row of k_rows / v_rows, else packed row `row`
+  int row;
+};
+constexpr TokenPlace token_place(int token, int total, int W, int S) {
+  return token >= total - W ? TokenPlace{true, token % W} : token < S ? TokenPlace{true, W + token} : TokenPlace{false, token - S};
+}
+
+// Attention: chunks of a sequence's rows.  A workgroup's wavefronts take every kPagedWaves-th tile of a chunk of packed
+// rows; chunks are whole tiles for each of them, at least two.
+constexpr int kPagedWaves = 4, kPagedTile = 32;
+constexpr int kPagedMinChunk = 2 * kPagedTile * kPagedWaves;
+constexpr int kPagedMaxSplits = 128;     // chunks of packed rows
+constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
+struct Chunks {
+  int n_kept, n_win, nq;    // sink rows, ring rows, packed rows
+  int rows, packed, chunk;  // chunks of full rows, of packed rows; packed rows per chunk
+};
+constexpr Chunks chunks_of(int total, int W, int S, int n_splits) {
+  Chunks c{0, total < W ? total : W, 0, 0, 0, kPagedMinChunk};
+  const int before = total - c.n_win;
+  c.n_kept = before < S ? before : S;
+  c.nq = before - c.n_kept;
+  c.rows = (c.n_win + c.n_kept + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk;
+  const int per = c.nq / n_splits + (c.nq % n_splits > 0), step = kPagedTile * kPagedWaves;
+  const int chunk = (per / step + (per % step > 0)) * step;
+  if (chunk > c.chunk) c.chunk = chunk;
+  c.packed = c.nq / c.chunk + (c.nq % c.chunk > 0);
+  return c;
+}
+constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
+
+// Whether a sequence's entry x of the page table can be followed.
+constexpr bool page_known(int x, int table_stride) { return x >= 0 && x < table_stride; }
+constexpr bool page_valid(int id, int n_pages) { return id >= 0 && id < n_pages; }
+
+}  // namespace skvq

@@ -1,0 +1,143 @@
+// Rotary positions, device side: cosine and sine of position * frequency, and the rotation of a pair.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "skvq.h"
+
+namespace skvq {
+
+// A rotation as kernels take it, by value: 1 KB of kernel arguments, so a rope object holds no device memory.
+struct RopeTable {
+  uint64_t turn[SKVQ_ROPE_MAX_HEAD_DIM / 2];  // per pair: turns per token, mod 1, in units of 2^-64
+  double amplitude;
+  int half;         // pairs (0: nothing is rotated)
+  int interleaved;  // pair i is channels (2i, 2i + 1), else (i, i + half)
+};
+
+// (cos, sin) of 2 pi * position * turn, times the amplitude, rounded to fp32.  position * turn wraps at 2^64,
+// which is one turn: no range reduction is left to do but the quadrant, at any position.  Series of sine to
+// x^13 and cosine to x^14 at |x| <= pi/4: the terms left out are below 2^-45, so the fp32 results are the
+// rounded true ones (but for about one in 2^20 next to a border).  Some 40 double operations per (token,
+// pair), shared by all heads.
+__device__ __forceinline__ float2 rope_cos_sin(uint64_t turn, int position, double amplitude) {
+  const uint64_t t = turn * (uint64_t)(int64_t)position;
+  const unsigned quadrant = (unsigned)((t + (1ull << 61)) >> 62);
+  const int64_t r = (int64_t)(t - ((uint64_t)quadrant << 62));  // [-1/8, 1/8) of a turn
+  const double x = (double)r * (6.283185307179586476925286766559 / 18446744073709551616.0);
+  const double z = x * x;
+  double s = 1.0 / 6227020800.0;
+  s = fma(s, z, -1.0 / 39916800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  s = fma(s, z, 1.0 / 120.0);
+  s = fma(s, z, -1.0 / 6.0);
+  s = fma(s * z, x, x);
+  double c = -1.0 / 87178291200.0;
+  c = fma(c, z, 1.0 / 479001600.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  c = fma(c, z, -1.0 / 720.0);
+  c = fma(c, z, 1.0 / 24.0);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const bool swap = quadrant & 1u;
+  const double cs = swap ? s : c, sn = swap ? c : s;
+  const bool neg_c = (quadrant + 1u) & 2u, neg_s = quadrant & 2u;
+  return make_float2((float)((neg_c ? -cs : cs) * amplitude), (float)((neg_s ? -sn : sn) * amplitude));
+}
+
+// One member of a rotated pair: x * c + other * s, each operation rounded once (the first member takes s
+// negated: a c - b s = a c + b (-s), the same three roundings).
+__device__ __forceinline__ float rope_turned(float x, float other, float c, float s) {
+#pragma clang fp contract(off)
+  const float p = x * c;
+  const float q = other * s;
+  return p + q;
+}
+
+// The rotation of a group of tokens by a workgroup of kRopeThreads.  cs: their cosines and sines, [token][pair],
+// in LDS.  rows(k, h, &from, &to): head h's rows of token k of the group, false where there is no such token.
+//
+// A thread keeps the cosines and sines of its place in the head in registers and walks over the heads, two
+// pieces of V channels (both members of V pairs) per step, kRopeAhead steps' loads in flight.
+constexpr int kRopeThreads = 256;
+constexpr int kRopeMaxTokens = 4;  // tokens per workgroup
+constexpr int kRopeAhead = 4;
+constexpr int kRopeMaxPairs = SKVQ_ROPE_MAX_HEAD_DIM / 2;
+
+template <class T, int V>
+struct alignas(sizeof(T) * V) Piece {
+  T v[V];
+};
+
+template <class T, int V, class Rows>
+__device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*cs)[kRopeMaxPairs], int n_here,
+                                          int head_dim, bool copy_rest, int n_heads, Rows rows) {
+  typedef Piece<T, V> P;
+  const int half = tab.half, rotated = half / V, pieces = rotated + (copy_rest ? (head_dim - 2 * half) / V : 0);
+  const int places = n_here * pieces, head_lanes = places < kRopeThreads ? kRopeThreads / places : 1;
+  for (int x = threadIdx.x; x < places * head_lanes; x += kRopeThreads) {
+    const int hl = x / places, place = x - hl * places;
+    const int k = place / pieces, j = place - k * pieces;
+    const bool turn = j < rotated;
+    // offsets of the two pieces; a piece that is copied has no second
+    int oa = j * V, ob = half + j * V;
+    if (tab.interleaved) {
+      oa = 2 * V * j;
+      ob = oa + V;
+    }
+    if (!turn) oa = ob = 2 * half + (j - rotated) * V;
+    float c[V], s[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float2 f = turn ? cs[k][j * V + e] : make_float2(1.0f, 0.0f);
+      c[e] = f.x;
+      s[e] = f.y;
+    }
+    for (int h0 = hl; h0 < n_heads; h0 += kRopeAhead * head_lanes) {
+      P pa[kRopeAhead], pb[kRopeAhead];
+      T *to[kRopeAhead];
+#pragma unroll
+      for (int u = 0; u < kRopeAhead; ++u) {
+        const int h = h0 + u * head_lanes;
+        const T *from;
+        to[u] = nullptr;
+        if (h < n_heads && rows(k, h, from, to[u])) {
+          pa[u] = *reinterpret_cast<const P *>(from + oa);
+          if (turn) pb[u] = *reinterpret_cast<const P *>(from + ob);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kRopeAhead; ++u)
+        if (to[u]) {
+          if (turn) {
+            P ra, rb;
+            if (V > 1 && tab.interleaved) {
+#pragma unroll
+              for (int e = 0; e + 1 < V; e += 2) {  // (pairs within a piece)
+                const int f = e / 2, g = V / 2 + e / 2;
+                ra.v[e] = (T)rope_turned((float)pa[u].v[e], (float)pa[u].v[e + 1], c[f], -s[f]);
+                ra.v[e + 1] = (T)rope_turned((float)pa[u].v[e + 1], (float)pa[u].v[e], c[f], s[f]);
+                rb.v[e] = (T)rope_turned((float)pb[u].v[e], (float)pb[u].v[e + 1], c[g], -s[g]);
+                rb.v[e + 1] = (T)rope_turned((float)pb[u].v[e + 1], (float)pb[u].v[e], c[g], s[g]);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                ra.v[e] = (T)rope_turned((float)pa[u].v[e], (float)pb[u].v[e], c[e], -s[e]);
+                rb.v[e] = (T)rope_turned((float)pb[u].v[e], (float)pa[u].v[e], c[e], s[e]);
+              }
+            }
+            *reinterpret_cast<P *>(to[u] + oa) = ra;
+            *reinterpret_cast<P *>(to[u] + ob) = rb;
+          } else {
+            *reinterpret_cast<P *>(to[u] + oa) = pa[u];
+          }
+        }
+    }
+  }
+}
+
+}  // namespace skvq

@@ -1,0 +1,521 @@
+"""The paged 4-bit cache against a plain one on the host: pages and rows byte for byte, rows read back, attention in 64
+bits with derived bounds; masks, windows, sinks, page sizes, ragged and empty batches, strides, device errors, captured
+calls; and a run of everything together."""
+import numpy as np
+import pytest
+import torch
+
+from paged_plain import D, PlainPaged
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2405_06219_amd import binding
+    return binding
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+class Both:
+    """The same cache as a PlainPaged and as a SkvqPagedCache, fed the same rows."""
+
+    def __init__(self, B, hq=4, hk=2, group=128, window=16, page=16, n_pages=64, max_seqs=4, max_tokens=64, sinks=0, meta="f16",
+                 dtype=torch.float16, seed=0, sm_scale=0.0):
+        self.B, self.rng = B, np.random.default_rng(seed)
+        self.hq, self.hk, self.dtype, self.sm = hq, hk, dtype, sm_scale
+        perm = [np.stack([self.rng.permutation(D) for _ in range(hk)]).astype(np.int32) for _ in range(2)]
+        clip = [self.rng.uniform(0.8, 1.0, (hk, D // group)).astype(np.float32) for _ in range(2)]
+        self.plain = PlainPaged(hk, group, window, page, n_pages, max_seqs, *perm, *clip, sinks=sinks, meta=meta, dtype=dtype)
+        self.gpu = B.SkvqPagedCache(hq, hk, group, window, page, n_pages, max_seqs, max_tokens, *perm, *clip, n_sink=sinks,
+                                    meta=meta, dtype=dtype, device=DEV, sm_scale=sm_scale)
+        for t in self.gpu.buffers.values():
+            t.fill_(0xAB)
+        self.size = [10 ** self.rng.uniform(-1, 0.5, (hk, D)) for _ in range(2)]
+        free = self.rng.permutation(n_pages)
+        per = n_pages // max_seqs
+        self.table = free[:per * max_seqs].reshape(max_seqs, per).astype(np.int32)
+        self.slots = self.rng.permutation(max_seqs).astype(np.int32)
+
+    def draw(self, n, heads, size=None):
+        x = self.rng.standard_normal((n, heads, D)) * (1 if size is None else size)
+        return torch.from_numpy(x.astype(np.float32)).to(self.dtype)
+
+    def lens(self, seqs):
+        return [self.plain.tokens[int(self.slots[i])][0].shape[0] if int(self.slots[i]) in self.plain.tokens else 0 for i in seqs]
+
+    def batch(self, seqs, new, lens=None, **kw):
+        cu = np.concatenate([[0], np.cumsum(new)])
+        return self.B.SkvqBatch(ints(cu), ints(self.lens(seqs) if lens is None else lens), ints(self.table[seqs]),
+                                slots=ints(self.slots[seqs]), n_tokens=kw.pop("n_tokens", int(cu[-1])), **kw)
+
+    def append(self, seqs, new):
+        n = int(sum(new))
+        k, v = self.draw(n, self.hk, self.size[0]), self.draw(n, self.hk, self.size[1])
+        at = 0
+        for i, m in zip(seqs, new):
+            self.plain.append(int(self.slots[i]), self.table[i], k[at:at + m].float().numpy(), v[at:at + m].float().numpy())
+            at += m
+        self.gpu.skvq_paged_append(self.batch(seqs, new), k.to(DEV), v.to(DEV))
+
+    def check_buffers(self):
+        torch.cuda.synchronize()
+        pages = self.gpu.buffers["pages"].cpu().numpy().reshape(self.plain.pages.shape)
+        assert np.array_equal(pages, self.plain.pages), np.argwhere(pages != self.plain.pages)[:4]
+        for name, want in zip(("k_rows", "v_rows"), self.plain.rows):
+            raw = self.gpu.buffers[name].view(self.dtype).cpu().float().numpy().reshape(want.shape)
+            there = np.broadcast_to(self.plain.written[:, None, :, None], want.shape)
+            assert np.array_equal(raw[there], want[there]), name
+            untouched = self.gpu.buffers[name].cpu().numpy().reshape(*want.shape[:3], 2 * D)[~there[..., 0]]
+            assert (untouched == 0xAB).all(), name
+        assert self.gpu.skvq_paged_errors() == 0
+
+    def attend(self, seqs, new, **kw):
+        n = int(sum(new))
+        q = self.draw(n, self.hq)
+        got = self.gpu.skvq_paged_attention(self.batch(seqs, new), q.to(DEV), **kw)
+        torch.cuda.synchronize()
+        want, bound, at = np.zeros((n, self.hq, D)), np.zeros((n, self.hq, D)), 0
+        for i, m in zip(seqs, new):
+            if m:
+                want[at:at + m], bound[at:at + m] = self.plain.attend(int(self.slots[i]), q[at:at + m].float().numpy(), self.sm or None)
+            at += m
+        return q, got, want, bound
+
+    def check_attention(self, seqs, new):
+        q, got, want, bound = self.attend(seqs, new)
+        off = np.abs(got.double().cpu().numpy() - want)
+        assert (off <= bound).all(), (float(off.max()), float((off / bound).max()))
+        return q, got
+
+
+FORMATS = [(128, "f16", torch.float16), (64, "e4m3", torch.bfloat16), (32, "f32", torch.float16), (128, "e4m3", torch.float16),
+           (64, "f16", torch.bfloat16), (32, "e4m3", torch.bfloat16), (128, "f32", torch.bfloat16), (64, "f32", torch.float16),
+           (32, "f16", torch.float16)]
+
+
+@pytest.mark.parametrize("group,meta,dtype", FORMATS)
+def test_append_read_attend(B, group, meta, dtype):
+    b = Both(B, hq=4, hk=2, group=group, meta=meta, dtype=dtype, sinks=3, seed=group)
+    seqs = [0, 1, 2, 3]
+    for new in ([1, 0, 19, 150], [0, 5, 1, 1], [40, 1, 0, 1], [1, 1, 1, 0]):   # prompts, single tokens, nothing
+        b.append(seqs, new)
+        b.check_buffers()
+        b.check_attention([i for i, n in zip(seqs, new) if n], [min(n, 6) for n in new if n])
+    # all of every sequence back, and parts
+    lens = b.lens(seqs)
+    for first, count in ((None, lens), ([0] * 4, lens), ([n // 3 for n in lens], [n // 2 for n in lens]), (lens, [0] * 4)):
+        kw = {} if first is None else {"first": ints(first)}
+        k, v = b.gpu.skvq_paged_read(b.batch(seqs, count, **kw))
+        at = 0
+        for i, n, f in zip(seqs, count, first or [0] * 4):
+            for got, want in zip((k, v), b.plain.read(int(b.slots[i]), f, n)):
+                assert np.array_equal(got[at:at + n].float().cpu().numpy(), want)
+            at += n
+    assert b.gpu.skvq_paged_errors() == 0
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (3, 2), (16, 1), (128, 4), (130, 0)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_windows_and_lengths(B, window, sinks, page):
+    b = Both(B, hq=3, hk=1, window=window, sinks=sinks, page=page, n_pages=90, max_seqs=2, seed=window)
+    for new in ([1, window], [1, 1], [2, 1], [window + 1, 0], [0, 3 * window + 70], [1, 33], [7, 1]):
+        b.append([0, 1], new)
+        b.check_buffers()
+        b.check_attention([1, 0], [min(2, b.lens([1])[0]), 1])
+
+
+@pytest.mark.parametrize("hq,hk", [(1, 1), (8, 1), (16, 1), (5, 5), (12, 4), (48, 3)])
+@pytest.mark.parametrize("new", [1, 3, 17])
+def test_heads_and_query_tokens(B, hq, hk, new):
+    # up to 17 x 16 rows of a kv head; with a window of 8 the later queries' limits lie among the packed rows
+    b = Both(B, hq=hq, hk=hk, window=8, sinks=2, page=32, n_pages=20, max_seqs=2, seed=hq + new)
+    b.append([0, 1], [300, 45])
+    b.check_attention([0, 1], [new, min(new, 2)])
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("total", [16 + 15, 16 + 16, 16 + 17, 16 + 255, 16 + 256, 16 + 257, 16 + 600])
+def test_pages_and_tiles_end_anywhere(B, page, total):
+    b = Both(B, page=page, n_pages=max(2, 2 * -(-total // page)), max_seqs=2, seed=page + total)
+    b.append([0, 1], [total, 1])
+    b.check_buffers()
+    b.check_attention([0], [1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("group", [128, 32])
+def test_long_contexts(B, dtype, group):
+    b = Both(B, hq=2, hk=1, group=group, dtype=dtype, window=100, page=64, n_pages=400, max_seqs=2, max_tokens=4, sinks=5, seed=5)
+    b.append([0, 1], [9001, 2500])
+    b.check_attention([0, 1], [2, 1])
+
+
+def test_values_without_spread_and_scores_far_apart(B):
+    # a scale of zero has no logarithm; one token takes all the weight, first, last or packed; the largest fp16 queries
+    b = Both(B, hq=2, hk=1, window=4, page=16, n_pages=16, max_seqs=1, seed=9, meta="f32")
+    n = 150
+    k, v = b.draw(n, 1), torch.zeros((n, 1, D), dtype=torch.float16)
+    v[:, 0] = torch.arange(n, dtype=torch.float16)[:, None] / 8
+    k[60] *= 30
+    b.plain.append(int(b.slots[0]), b.table[0], k.float().numpy(), v.float().numpy())
+    b.gpu.skvq_paged_append(b.batch([0], [n]), k.to(DEV), v.to(DEV))
+    b.check_buffers()
+    for factor in (1.0, 30.0, 0.0):
+        draw = b.draw
+        b.draw = lambda *a, **kw: (draw(*a, **kw).float() * factor).half()
+        b.check_attention([0], [1])
+        b.draw = draw
+
+
+def test_small_values_keep_their_precision(B):
+    # scales of 1e-5 beside weights of 1e-3: their product is far below fp16's normal numbers
+    b = Both(B, hq=2, hk=1, window=4, page=16, n_pages=64, max_seqs=1, seed=10, meta="f32", dtype=torch.bfloat16)
+    b.size = [np.full((1, D), 1.0), np.full((1, D), 1e-4)]
+    b.append([0], [900])
+    q, got, want, bound = b.attend([0], [1])
+    off = np.abs(got.double().cpu().numpy() - want)
+    assert (off <= bound - 1e-7 + 1e-12).all()
+
+
+def test_garbage_where_no_token_is(B):
+    # NaN patterns in every byte that no token has written: pages, rows and workspace
+    for meta, dtype in (("f16", torch.float16), ("f32", torch.bfloat16), ("e4m3", torch.float16)):
+        b = Both(B, window=20, sinks=6, meta=meta, dtype=dtype, seed=11)
+        for t in b.gpu.buffers.values():
+            t.fill_(0xFF)
+        b.append([0, 1, 2], [9, 47, 1])
+        b.check_attention([0, 1, 2], [2, 1, 1])
+        assert b.gpu.skvq_paged_errors() == 0
+
+
+def test_rows_of_other_strides_and_rows_behind_the_last(B):
+    b = Both(B, hq=4, hk=2, seed=12)
+    b.append([0, 1], [50, 30])
+    rows = torch.from_numpy(b.rng.standard_normal((7, 8, D)).astype(np.float32)).half().to(DEV)
+    q, k, v = rows[:, :4], rows[:, 4:6], rows[:, 6:]
+    at = 0
+    for i, m in ((0, 3), (1, 2)):
+        b.plain.append(int(b.slots[i]), b.table[i], k[at:at + m].float().cpu().numpy(), v[at:at + m].float().cpu().numpy())
+        at += m
+    batch = b.batch([0, 1], [3, 2], n_tokens=7)              # two rows more than the sequences have
+    out_q = torch.full((7, 9, D), 5.0, dtype=torch.float16, device=DEV)
+    got = b.gpu.skvq_paged_append(batch, k, v, q=q, out_q=out_q[:, 2:6])
+    assert torch.equal(got[:5], q[:5]) and bool((out_q[5:] == 5).all()) and bool((out_q[:, :2] == 5).all()) and bool((out_q[:, 6:] == 5).all())
+    b.check_buffers()
+    wide = torch.full((7, 9, D), 5.0, dtype=torch.float16, device=DEV)
+    f32 = torch.full((7, 4, D), 5.0, device=DEV)
+    dense = b.gpu.skvq_paged_attention(b.batch([0, 1], [3, 2]), q[:5].contiguous())
+    b.gpu.skvq_paged_attention(batch, q, out=wide[:, 1:5], out_f32=f32)
+    assert torch.equal(wide[:5, 1:5], dense) and torch.equal(f32[:5].half(), dense)
+    assert bool((wide[5:] == 5).all()) and bool((wide[:, 0] == 5).all()) and bool((wide[:, 5:] == 5).all()) and bool((f32[5:] == 5).all())
+    assert b.gpu.skvq_paged_attention(batch, q, out_f32=f32) is f32
+    kv = torch.full((7, 5, D), 5.0, dtype=torch.float16, device=DEV)
+    k2, _ = b.gpu.skvq_paged_read(batch, out_k=kv[:, 3:])
+    dense_k, _ = b.gpu.skvq_paged_read(b.batch([0, 1], [3, 2]))
+    assert torch.equal(k2[:5], dense_k) and bool((kv[5:] == 5).all()) and bool((kv[:, :3] == 5).all())
+    assert b.gpu.skvq_paged_errors() == 0
+
+
+@pytest.mark.parametrize("layout,rotary", [("half", 128), ("interleaved", 128), ("half", 64), ("half", 20), ("interleaved", 20)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("given", [False, True])
+def test_rotation_on_the_way_is_the_rotation(B, layout, rotary, dtype, given):
+    # appending with a rotation is appending what skvq_rope_apply gives, bit for bit; the queries too
+    b, c = (Both(B, hq=4, hk=2, sinks=2, dtype=dtype, seed=13) for _ in range(2))
+    rope = B.SkvqRope(128, rotary, layout, scaling="ntk", factor=4.0)
+    for new in ([70, 1], [1, 33], [1, 1]):
+        n = sum(new)
+        lens = [a + x for a, x in zip(b.lens([0, 1]), new)]
+        k, v, q = (b.draw(n, h).to(DEV) for h in (2, 2, 4))
+        if given:
+            at = np.concatenate([b.rng.integers(-50, 1 << 20, m) for m in new]).astype(np.int32)
+        else:
+            at = np.concatenate([np.arange(t - m, t) for t, m in zip(lens, new)]).astype(np.int32)
+        rk, rq = (rope.skvq_rope_apply(x[None], positions=ints(at))[0] for x in (k, q))
+        i = 0
+        for s, m in enumerate(new):
+            b.plain.append(int(b.slots[s]), b.table[s], rk[i:i + m].float().cpu().numpy(), v[i:i + m].float().cpu().numpy())
+            i += m
+        kw = {"positions": ints(at)} if given else {}
+        out_q = b.gpu.skvq_paged_append(b.batch([0, 1], new, **kw), k, v, rope=rope, q=q)
+        assert torch.equal(out_q, rq)
+        again = q.clone()
+        c.gpu.skvq_paged_append(b.batch([0, 1], new, **kw), k, v, rope=rope, q=again, out_q=again)   # in place
+        assert torch.equal(again, rq)
+        b.check_buffers()
+        for name in ("pages", "k_rows", "v_rows"):
+            assert torch.equal(b.gpu.buffers[name], c.gpu.buffers[name])
+
+
+def test_shared_pages_and_batches_in_any_order(B):
+    # a common prefix in shared pages, each sequence its own window: both read it
+    b = Both(B, window=8, page=16, n_pages=32, max_seqs=2, seed=14)
+    b.append([0], [80])
+    b.table[1, :4] = b.table[0, :4]
+    slot0, slot1 = int(b.slots[0]), int(b.slots[1])
+    b.plain.tokens[slot1] = [x.copy() for x in b.plain.tokens[slot0]]
+    for name in ("k_rows", "v_rows"):
+        rows = b.gpu.buffers[name].view(torch.float16).view(2, b.hk, 8, D)
+        rows[slot1] = rows[slot0]
+    b.table[1, 4] = b.table[1, 5]         # packed rows 64 .. 71 in a page of its own
+    pages = b.gpu.buffers["pages"].view(b.plain.pages.shape)
+    pages[int(b.table[1, 4])] = pages[int(b.table[0, 4])]
+    b.append([1, 0], [3, 9])
+    b.check_attention([0, 1], [1, 2])
+    q, one = b.check_attention([1, 0], [2, 1])
+    alone = b.gpu.skvq_paged_attention(b.batch([1], [2]), q[:2].to(DEV))
+    assert torch.equal(alone, one[:2])    # what else is in the batch changes nothing
+
+
+def test_more_sequences_than_lanes(B):
+    # 70 and 200 sequences, most of them of a token or two, some with nothing new
+    for seqs, seed in ((70, 15), (200, 16)):
+        b = Both(B, hq=2, hk=1, window=2, page=16, n_pages=2 * seqs, max_seqs=seqs, max_tokens=2 * seqs, seed=seed)
+        every = list(range(seqs))
+        b.append(every, [int(x) for x in b.rng.integers(1, 30, seqs)])
+        new = [int(x) for x in b.rng.integers(0, 3, seqs)]
+        b.append(every, new)
+        b.check_buffers()
+        b.check_attention(every, [min(n, 1) for n in new])
+
+
+def test_device_errors(B):
+    """Entries that lead out of the buffers are left out and reported; everything else is as it would be without them."""
+    def fresh():
+        b = Both(B, window=8, page=16, n_pages=16, max_seqs=4, seed=17)
+        b.append([0, 1, 2], [60, 61, 62])
+        return b
+    b = fresh()
+    q = b.draw(3, 4).to(DEV)
+    want = b.gpu.skvq_paged_attention(b.batch([0, 1, 2], [1, 1, 1]), q)
+    nan = float("nan")
+    for bad, lens, slots, table, bits in [
+            (1, [60, 61, 62], None, (1, 2, -1), B.SKVQ_PAGED_BAD_PAGE), (1, [60, 61, 62], None, (1, 0, 16), B.SKVQ_PAGED_BAD_PAGE),
+            (2, [60, 61, 62 + 1000], None, None, B.SKVQ_PAGED_BAD_PAGE),     # more tokens than the table has pages for
+            (0, [60, 61, 62], [-1, None, None], None, B.SKVQ_PAGED_BAD_SLOT), (2, [60, 61, 62], [None, None, 4], None, B.SKVQ_PAGED_BAD_SLOT)]:
+        t, s = b.table[:3].copy(), b.slots[:3].copy()
+        if table:
+            t[table[0], table[1]] = table[2]
+        if slots:
+            s = np.array([x if y is None else y for x, y in zip(s, slots)], np.int32)
+        batch = B.SkvqBatch(ints([0, 1, 2, 3]), ints(lens), ints(t), slots=ints(s), n_tokens=3)
+        got = b.gpu.skvq_paged_attention(batch, q)
+        assert b.gpu.skvq_paged_errors() == bits and b.gpu.skvq_paged_errors() == 0
+        for i in range(3):
+            assert bool(torch.isnan(got[i]).all()) if i == bad else torch.equal(got[i], want[i]), (bad, i)
+    # counts: nothing of the sequence is touched
+    for cu, lens, bad in [([0, 1, 0, 1], [60, 61, 62], 1), ([0, 1, 2, 9], [60, 61, 62], 2), ([0, 1, 2, 3], [60, 61, 0], 2), ([0, 1, 2, 3], [60, -5, 62], 1),
+                          ([0, 1, 2, 3], [60, 61, 2 ** 31 - 1], 2), ([-3, 1, 2, 3], [60, 61, 62], 0)]:
+        got = torch.full((3, 4, D), 9.0, dtype=torch.float16, device=DEV)
+        batch = B.SkvqBatch(ints(cu), ints(lens), ints(b.table[:3]), slots=ints(b.slots[:3]), n_tokens=3)
+        b.gpu.skvq_paged_attention(batch, q, out=got)
+        assert b.gpu.skvq_paged_errors() & B.SKVQ_PAGED_BAD_COUNTS
+        assert not bool(torch.isnan(got).any())
+    # an append: the bad sequence's pages and rows stay, the others' are written
+    for table, slots, lens, bits, bad in [((1, 3, 99), None, [63, 64, 65], B.SKVQ_PAGED_BAD_PAGE, 1), (None, [None, 7, None], [63, 64, 65], B.SKVQ_PAGED_BAD_SLOT, 1),
+                                          (None, None, [63, 64, 2], B.SKVQ_PAGED_BAD_COUNTS, 2)]:
+        b, c = fresh(), fresh()
+        t, s = b.table[:3].copy(), b.slots[:3].copy()
+        if table:
+            t[table[0], table[1]] = table[2]
+        if slots:
+            s = np.array([x if y is None else y for x, y in zip(s, slots)], np.int32)
+        k, v = b.draw(9, 2), b.draw(9, 2)
+        batch = B.SkvqBatch(ints([0, 3, 6, 9]), ints(lens), ints(t), slots=ints(s), n_tokens=9)
+        b.gpu.skvq_paged_append(batch, k.to(DEV), v.to(DEV))
+        assert b.gpu.skvq_paged_errors() == bits
+        for i in range(3):
+            if i != bad:
+                b.plain.append(int(s[i]), t[i], k[3 * i:3 * i + 3].float().numpy(), v[3 * i:3 * i + 3].float().numpy())
+        if bits == B.SKVQ_PAGED_BAD_PAGE:   # (its rows enter the window all the same; what left for the page is left out)
+            b.plain.append(int(s[1]), t[1], k[3:6].float().numpy(), v[3:6].float().numpy())
+        b.check_buffers()
+    # a read out of the sequence's tokens, or from a page that is none
+    b = fresh()
+    for first, count, table, bits in [([0, 60, 0], [1, 3, 1], None, B.SKVQ_PAGED_BAD_RANGE), ([0, -1, 0], [1, 1, 1], None, B.SKVQ_PAGED_BAD_RANGE),
+                                      ([0, 20, 0], [1, 4, 1], (1, 1, 16), B.SKVQ_PAGED_BAD_PAGE)]:
+        t = b.table[:3].copy()
+        if table:
+            t[table[0], table[1]] = table[2]
+        n = sum(count)
+        k, v = (torch.full((n, 2, D), 9.0, dtype=torch.float16, device=DEV) for _ in range(2))
+        batch = B.SkvqBatch(ints(np.concatenate([[0], np.cumsum(count)])), ints([60, 61, 62]), ints(t), slots=ints(b.slots[:3]), first=ints(first), n_tokens=n)
+        b.gpu.skvq_paged_read(batch, out_k=k, out_v=v)
+        assert b.gpu.skvq_paged_errors() == bits
+        assert bool((k[1:n - 1] == 9).all()) and bool((v[1:n - 1] == 9).all())
+        for got, x in zip((k, v), b.plain.read(int(b.slots[0]), 0, 1)):
+            assert np.array_equal(got[:1].float().cpu().numpy(), x)
+
+
+def test_refusals_of_calls(B):
+    b = Both(B, max_tokens=4, seed=18)
+    b.append([0, 1], [3, 2])
+    k, q = b.draw(5, 2).to(DEV), b.draw(5, 4).to(DEV)
+    batch = b.batch([0, 1], [3, 2])
+    for call in (lambda: b.gpu.skvq_paged_append(batch, k, k.float()), lambda: b.gpu.skvq_paged_append(batch, k[:4], k),
+                 lambda: b.gpu.skvq_paged_append(batch, k, k.cpu()), lambda: b.gpu.skvq_paged_append(batch, q, k),
+                 lambda: b.gpu.skvq_paged_attention(batch, k), lambda: b.gpu.skvq_paged_attention(batch, q, out=q.float()),
+                 lambda: b.gpu.skvq_paged_attention(batch, q, out_f32=q), lambda: b.gpu.skvq_paged_read(batch, out_k=q),
+                 lambda: B.SkvqBatch(ints([0, 1]).long(), ints([1]), ints([[0]])), lambda: B.SkvqBatch(ints([0]), ints([1]), ints([[0]]), n_tokens=1),
+                 lambda: B.SkvqBatch(ints([0, 1]), ints([1]), ints([0]), n_tokens=1),
+                 lambda: B.SkvqBatch(ints([0, 1]), ints([1]), ints([[0]]), slots=ints([0, 1]), n_tokens=1),
+                 lambda: B.SkvqPagedCache(4, 2, 128, 16, 16, 8, 2, 2, np.tile(np.arange(D), (2, 1)), np.tile(np.arange(D), (2, 1)), np.ones((2, 1)),
+                                          np.ones((2, 1)), buffers={"pages": torch.zeros(16, dtype=torch.uint8, device=DEV)})):
+        with pytest.raises(ValueError):
+            call()
+    rope = B.SkvqRope(64)
+    many = B.SkvqBatch(ints(np.arange(6)), ints([1] * 5), ints(np.zeros((5, 1))), n_tokens=5)    # five sequences, four slots
+    for call in (lambda: b.gpu.skvq_paged_attention(batch, q),                          # more query tokens than max_tokens
+                 lambda: b.gpu.skvq_paged_append(batch, k, k, rope=rope),               # another head's width
+                 lambda: b.gpu.skvq_paged_append(many, k, k),
+                 lambda: b.gpu.skvq_paged_append(batch, torch.zeros(5 * 260 + 1, dtype=torch.float16, device=DEV)[1:].view(5, 260)[:, :256].view(5, 2, D), k),
+                 lambda: b.gpu.skvq_paged_append(batch, torch.zeros(5 * 260, dtype=torch.float16, device=DEV).view(5, 260)[:, :256].view(5, 2, D), k)):
+        with pytest.raises(B.SkvqError) as e:
+            call()
+        assert e.value.status == B.SKVQ_ERR_INVALID_ARG
+    # nothing to do
+    none = b.batch([0, 1], [0, 0])
+    b.gpu.skvq_paged_append(none, k[:0], k[:0], q=q[:0])
+    assert b.gpu.skvq_paged_attention(none, q[:0]).shape == (0, 4, D) and b.gpu.skvq_paged_read(none)[0].shape == (0, 2, D)
+    empty = B.SkvqBatch(ints([0]), ints(np.zeros(0)), ints(np.zeros((0, 1))), n_tokens=0)
+    b.gpu.skvq_paged_append(empty, k[:0], k[:0])
+    b.check_buffers()
+
+
+def test_another_stream_and_the_same_bits_every_time(B):
+    b = Both(B, hq=8, hk=2, n_pages=400, page=16, max_seqs=2, window=32, seed=19)
+    b.append([0, 1], [2500, 700])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    q = b.draw(2, 8).to(DEV)
+    batch = b.batch([0, 1], [1, 1])
+    want = b.gpu.skvq_paged_attention(batch, q)
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = b.gpu.skvq_paged_attention(batch, q, stream=side)
+        side.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_captured_decode_steps(B):
+    """Append and attention captured once, replayed with the lengths, tokens and pages changed in between, against the same
+    steps called one by one."""
+    rope = B.SkvqRope(128)
+    b, c = (Both(B, hq=4, hk=2, window=8, sinks=1, n_pages=24, page=16, max_seqs=3, seed=20) for _ in range(2))
+    for x in (b, c):
+        x.append([0, 1, 2], [20, 3, 90])
+    lens = ints([20, 3, 90])
+    cu, table, slots = ints([0, 1, 2, 3]), ints(b.table), ints(b.slots)
+    batch = B.SkvqBatch(cu, lens, table, slots=slots, n_tokens=3)
+    k, v, q = (torch.zeros((3, h, D), dtype=torch.float16, device=DEV) for h in (2, 2, 4))
+    rq, out = torch.empty_like(q), torch.empty_like(q)
+
+    def step(cache):
+        cache.skvq_paged_append(batch, k, v, rope=rope, q=q, out_q=rq)
+        cache.skvq_paged_attention(batch, rq, out=out)
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        step(b.gpu)
+        graph.capture_end()
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(12):
+        lens.add_(1)
+        for t, h in ((k, 2), (v, 2), (q, 4)):
+            t.copy_(b.draw(3, h))
+        step(c.gpu)
+        want = out.clone()
+        out.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        for name in ("pages", "k_rows", "v_rows"):
+            assert torch.equal(b.gpu.buffers[name], c.gpu.buffers[name]), (i, name)
+    assert b.gpu.skvq_paged_errors() == 0
+
+
+def test_paged_rows_stand_for_what_the_fixed_cache_holds(B):
+    """The same keys and values in a SkvqCache of equal-length sequences and in pages: attention agrees within both bounds."""
+    rng = np.random.default_rng(21)
+    hq, hk, T, W, S = 8, 2, 700, 64, 4
+    perm = [np.stack([rng.permutation(D) for _ in range(hk)]).astype(np.int32) for _ in range(2)]
+    clip = np.full((hk, 2), 0.95, np.float32)
+    fixed = B.SkvqCache(2, hq, hk, 64, 4.0, W, 1024, *perm, clip, clip, k_bits=4.0, n_sink=S, meta="e4m3", device=DEV)
+    paged = B.SkvqPagedCache(hq, hk, 64, W, 32, 64, 2, 2, *perm, clip, clip, n_sink=S, meta="e4m3", device=DEV)
+    k, v = (torch.from_numpy(rng.standard_normal((2, hk, T, D)).astype(np.float16)).to(DEV) for _ in range(2))
+    q = torch.from_numpy(rng.standard_normal((2, hq, D)).astype(np.float16)).to(DEV)
+    fixed.skvq_prefill_quantize(k, v)
+    want = fixed.skvq_decode_attention(q)
+    table = ints(rng.permutation(64)[:50].reshape(2, 25))
+    rows = [x.transpose(1, 2).reshape(2 * T, hk, D) for x in (k, v)]
+    paged.skvq_paged_append(B.SkvqBatch(ints([0, T, 2 * T]), ints([T, T]), table, n_tokens=2 * T), *rows)
+    out = torch.empty((2, hq, D), device=DEV)
+    paged.skvq_paged_attention(B.SkvqBatch(ints([0, 1, 2]), ints([T, T]), table, n_tokens=2), q, out_f32=out)
+    # the fixed cache's own bound, and fp16 weights (2^-11) of values up to 4 about their middle
+    assert float((out - want).abs().max()) <= 2e-3 + 4 * 2.0 ** -11
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_a_server_s_run(B, dtype):
+    """Prompts of different lengths rotated, attended to and appended, decode steps of all sequences with a verification of
+    several tokens between them, one sequence read out and put into another cache: as a server uses them together."""
+    rng = np.random.default_rng(22)
+    hq, hk, W, S, P = 8, 2, 32, 2, 16
+    perm = [np.stack([rng.permutation(D) for _ in range(hk)]).astype(np.int32) for _ in range(2)]
+    clip = np.full((hk, 1), 0.97, np.float32)
+    cache = B.SkvqPagedCache(hq, hk, 128, W, P, 60, 3, 16, *perm, clip, clip, n_sink=S, dtype=dtype, device=DEV)
+    plain = PlainPaged(hk, 128, W, P, 60, 3, *perm, clip, clip, sinks=S, dtype=dtype)
+    rope = B.SkvqRope(128, scaling="bands", factor=4.0, original_context=64, low=1.0, high=4.0)
+    table_h = rng.permutation(60).reshape(3, 20).astype(np.int32)
+    table, lens = ints(table_h), [0, 0, 0]
+
+    def step(new):
+        n = sum(new)
+        rows = torch.from_numpy(rng.standard_normal((n, hq + 2 * hk, D)).astype(np.float32)).to(dtype).to(DEV)
+        for i, m in enumerate(new):
+            lens[i] += m
+        batch = B.SkvqBatch(ints(np.concatenate([[0], np.cumsum(new)])), ints(lens), table, n_tokens=n)
+        q = cache.skvq_paged_append(batch, rows[:, hq:hq + hk], rows[:, hq + hk:], rope=rope, q=rows[:, :hq])
+        at = 0
+        for i, m in enumerate(new):
+            pos = ints(np.arange(lens[i] - m, lens[i]))
+            if m:
+                rk = rope.skvq_rope_apply(rows[None, at:at + m, hq:hq + hk], positions=pos)[0]
+                plain.append(i, table_h[i], rk.float().cpu().numpy(), rows[at:at + m, hq + hk:].float().cpu().numpy())
+            at += m
+        return batch, q
+
+    step([120, 7, 33])
+    for new in ([1, 1, 1], [4, 0, 2], [1, 1, 0], [1, 1, 1]):
+        batch, q = step(new)
+        got = cache.skvq_paged_attention(batch, q).double().cpu().numpy()
+        at = 0
+        for i, m in enumerate(new):
+            if m:
+                want, bound = plain.attend(i, q[at:at + m].float().cpu().numpy())
+                assert (np.abs(got[at:at + m] - want) <= bound).all()
+            at += m
+    # sequence 0 moves into a cache of another page size and the widest pairs; it attends there as its rows say
+    k, v = cache.skvq_paged_read(B.SkvqBatch(ints([0, lens[0]]), ints([lens[0]]), table[:1], n_tokens=lens[0]))
+    for got, want in zip((k, v), plain.read(0, 0, lens[0])):
+        assert np.array_equal(got.float().cpu().numpy(), want)
+    other = B.SkvqPagedCache(hq, hk, 128, W, 64, 4, 1, 4, *perm, clip, clip, n_sink=S, meta="f32", dtype=dtype, device=DEV)
+    moved = PlainPaged(hk, 128, W, 64, 4, 1, *perm, clip, clip, sinks=S, meta="f32", dtype=dtype)
+    t2 = np.arange(4, dtype=np.int32)[None]
+    batch = B.SkvqBatch(ints([0, lens[0]]), ints([lens[0]]), ints(t2), n_tokens=lens[0])
+    other.skvq_paged_append(batch, k, v)
+    moved.append(0, t2[0], k.float().cpu().numpy(), v.float().cpu().numpy())
+    q = torch.from_numpy(rng.standard_normal((1, hq, D)).astype(np.float32)).to(dtype)
+    got = other.skvq_paged_attention(B.SkvqBatch(ints([0, 1]), ints([lens[0]]), ints(t2), n_tokens=1), q.to(DEV))
+    want, bound = moved.attend(0, q.float().numpy())
+    assert (np.abs(got.double().cpu().numpy() - want) <= bound).all()
+    assert cache.skvq_paged_errors() == 0 and other.skvq_paged_errors() == 0
