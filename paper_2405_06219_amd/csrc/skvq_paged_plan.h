@@ -13,7 +13,6 @@ struct UnitDeal {
 constexpr UnitDeal kAppendDeal{1, 2, 3};
 constexpr UnitDeal kReadDeal{1, 2, 2};
 constexpr UnitDeal kTokenDeal{1, 0, 0};
-constexpr UnitDeal row_deal(int query_heads) { return UnitDeal{query_heads, 4, 1}; }  // blocks of 16 query rows
 constexpr long long unit_start(const UnitDeal &d, int row0, int i) {
   return (((long long)row0 * d.mul) >> d.div_log2) + (long long)i * d.pad;
 }
@@ -78,29 +77,45 @@ constexpr TokenPlace token_place(int token, int total, int W, int S) {
   return token >= total - W ? TokenPlace{true, token % W} : token < S ? TokenPlace{true, W + token} : TokenPlace{false, token - S};
 }
 
-// Attention: chunks of a sequence's rows.  A workgroup's wavefronts take every kPagedWaves-th tile of a chunk of packed
-// rows; chunks are whole tiles for each of them, at least two.
+// Attention: the rows of a sequence are cut into chunks of full-precision rows and chunks of packed rows, each read by a
+// workgroup per (block of 16 query rows, kv head): a unit.  A workgroup's wavefronts take every kPagedWaves-th tile of a
+// chunk of packed rows; chunks are whole tiles for each of them, at least two.
 constexpr int kPagedWaves = 4, kPagedTile = 32;
-constexpr int kPagedMinChunk = 2 * kPagedTile * kPagedWaves;
-constexpr int kPagedMaxSplits = 128;     // chunks of packed rows
+constexpr int kPagedStep = kPagedTile * kPagedWaves;
+constexpr int kPagedMinChunk = 2 * kPagedStep;
+constexpr int kPagedMaxSplits = 128;     // chunks of packed rows of a sequence
 constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
+constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
+constexpr int whole_steps(int rows) { return (rows / kPagedStep + (rows % kPagedStep > 0)) * kPagedStep; }
+// Lengths are known on the device only, so every workgroup of a launch of `groups` finds the batch's chunk size from two
+// sums over the batch, per kv head: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a
+// chunk of full rows and a last, shorter chunk of packed ones per block).  The units fit `rounds` rounds over the
+// groups: as few as keep a chunk within 4096 rows, more where the extra units would fill half of them.
+constexpr int chunk_for(long long work, long long extra, int heads, int groups) {
+  work = (work < 1ll << 45 ? work : 1ll << 45) * heads;  // (beyond, a chunk is as long as it can be)
+  extra = (extra < 1ll << 40 ? extra : 1ll << 40) * heads;
+  long long rounds = work / (4096ll * groups) + 1;
+  const long long full = (2 * extra + groups - 1) / groups;
+  if (rounds < full) rounds = full;
+  const long long units = rounds * groups - extra, rows = (work + units - 1) / units;
+  const int chunk = whole_steps(rows < 0x40000000 ? (int)rows : 0x40000000);
+  return chunk < kPagedMinChunk ? kPagedMinChunk : chunk;
+}
 struct Chunks {
   int n_kept, n_win, nq;    // sink rows, ring rows, packed rows
   int rows, packed, chunk;  // chunks of full rows, of packed rows; packed rows per chunk
 };
-constexpr Chunks chunks_of(int total, int W, int S, int n_splits) {
-  Chunks c{0, total < W ? total : W, 0, 0, 0, kPagedMinChunk};
+constexpr Chunks chunks_of(int total, int W, int S, int chunk) {
+  Chunks c{0, total < W ? total : W, 0, 0, 0, chunk};
   const int before = total - c.n_win;
   c.n_kept = before < S ? before : S;
   c.nq = before - c.n_kept;
   c.rows = (c.n_win + c.n_kept + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk;
-  const int per = c.nq / n_splits + (c.nq % n_splits > 0), step = kPagedTile * kPagedWaves;
-  const int chunk = (per / step + (per % step > 0)) * step;
-  if (chunk > c.chunk) c.chunk = chunk;
+  const int least = whole_steps(c.nq / kPagedMaxSplits + (c.nq % kPagedMaxSplits > 0));  // (partials have room for so many)
+  if (least > c.chunk) c.chunk = least;
   c.packed = c.nq / c.chunk + (c.nq % c.chunk > 0);
   return c;
 }
-constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
 
 // Whether a sequence's entry x of the page table can be followed.
 constexpr bool page_known(int x, int table_stride) { return x >= 0 && x < table_stride; }

@@ -109,7 +109,7 @@ __device__ __forceinline__ Piece<T, 8> rotated(const RopeTable &tab, const LaneR
   Piece<T, 8> other, y;
   if (tab.interleaved) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) other.v[e] = x.v[e ^ 1];
+    for (int e = 0; e < 8; ++e) other[e] = x[e ^ 1];
   } else {
     *reinterpret_cast<Piece<T, 8> *>(row + 8 * m) = x;
     wave_lds_sync();
@@ -121,7 +121,7 @@ __device__ __forceinline__ Piece<T, 8> rotated(const RopeTable &tab, const LaneR
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int c = ch + e;
-        other.v[e] = row[c < half ? c + half : c < 2 * half ? c - half : c];
+        other[e] = row[c < half ? c + half : c < 2 * half ? c - half : c];
       }
     }
     wave_lds_sync();
@@ -129,8 +129,8 @@ __device__ __forceinline__ Piece<T, 8> rotated(const RopeTable &tab, const LaneR
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int ch = 8 * m + e;
-    const T z = (T)rope_turned((float)x.v[e], (float)other.v[e], t.c[e], t.s[e]);
-    y.v[e] = ch < 2 * tab.half ? z : x.v[e];
+    const T z = (T)rope_turned((float)x[e], (float)other[e], t.c[e], t.s[e]);
+    y[e] = ch < 2 * tab.half ? z : x[e];
   }
   return y;
 }
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedL
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
     T *head_rows = rows + (long long)h * (L.W + L.S) * kD + 8 * m;
-    P fresh{}, gone{};
+    P fresh = {}, gone = {};
     if (x.valid) {
       fresh = *reinterpret_cast<const P *>((const T *)src.p + token * src.stride + h * kD + 8 * m);
       if (x.old) gone = *reinterpret_cast<const P *>(head_rows + (long long)x.ring * kD);
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kRopeThreads) void paged_read_kernel(const PagedLay
   T *row = parked[wave][r];
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
-    P x{};
+    P x = {};
     if (valid && full) x = *reinterpret_cast<const P *>(rows + ((long long)h * (L.W + L.S) + at.row) * kD + 8 * m);
     if (valid && !full) {
       const uint8_t *part = page + (long long)h * L.part_bytes;

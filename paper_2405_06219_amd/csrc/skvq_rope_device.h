@@ -67,10 +67,10 @@ constexpr int kRopeMaxTokens = 4;  // tokens per workgroup
 constexpr int kRopeAhead = 4;
 constexpr int kRopeMaxPairs = SKVQ_ROPE_MAX_HEAD_DIM / 2;
 
+// V values as one access.  (A vector type: a struct around an array may be moved to LDS by the compiler, whose addressing
+// then waits for the dispatch packet in host memory, 10 us a launch.)
 template <class T, int V>
-struct alignas(sizeof(T) * V) Piece {
-  T v[V];
-};
+using Piece = T __attribute__((ext_vector_type(V)));
 
 template <class T, int V, class Rows>
 __device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*cs)[kRopeMaxPairs], int n_here,
@@ -118,16 +118,16 @@ __device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*c
 #pragma unroll
               for (int e = 0; e + 1 < V; e += 2) {  // (pairs within a piece)
                 const int f = e / 2, g = V / 2 + e / 2;
-                ra.v[e] = (T)rope_turned((float)pa[u].v[e], (float)pa[u].v[e + 1], c[f], -s[f]);
-                ra.v[e + 1] = (T)rope_turned((float)pa[u].v[e + 1], (float)pa[u].v[e], c[f], s[f]);
-                rb.v[e] = (T)rope_turned((float)pb[u].v[e], (float)pb[u].v[e + 1], c[g], -s[g]);
-                rb.v[e + 1] = (T)rope_turned((float)pb[u].v[e + 1], (float)pb[u].v[e], c[g], s[g]);
+                ra[e] = (T)rope_turned((float)pa[u][e], (float)pa[u][e + 1], c[f], -s[f]);
+                ra[e + 1] = (T)rope_turned((float)pa[u][e + 1], (float)pa[u][e], c[f], s[f]);
+                rb[e] = (T)rope_turned((float)pb[u][e], (float)pb[u][e + 1], c[g], -s[g]);
+                rb[e + 1] = (T)rope_turned((float)pb[u][e + 1], (float)pb[u][e], c[g], s[g]);
               }
             } else {
 #pragma unroll
               for (int e = 0; e < V; ++e) {
-                ra.v[e] = (T)rope_turned((float)pa[u].v[e], (float)pb[u].v[e], c[e], -s[e]);
-                rb.v[e] = (T)rope_turned((float)pb[u].v[e], (float)pa[u].v[e], c[e], s[e]);
+                ra[e] = (T)rope_turned((float)pa[u][e], (float)pb[u][e], c[e], -s[e]);
+                rb[e] = (T)rope_turned((float)pb[u][e], (float)pa[u][e], c[e], s[e]);
               }
             }
             *reinterpret_cast<P *>(to[u] + oa) = ra;

@@ -32,8 +32,8 @@ extern "C" int append_units(int total, int n_new, int W, int S) {
   const AppendPlan p = append_plan(total, n_new, W, S);
   return p.leaving_fours + p.vacant_fours;
 }
-extern "C" long long start_of(int kind, int heads, int row0, int i) {
-  return unit_start(kind == 0 ? kAppendDeal : kind == 1 ? kReadDeal : kind == 2 ? kTokenDeal : row_deal(heads), row0, i);
+extern "C" long long start_of(int kind, int row0, int i) {
+  return unit_start(kind == 0 ? kAppendDeal : kind == 1 ? kReadDeal : kTokenDeal, row0, i);
 }
 extern "C" int fours_to_read(int first, int n, int S) { return read_fours(first, n, S); }
 extern "C" int token_to_read(int first, int S, int unit, int r) { return read_token(first, S, unit, r); }
@@ -41,8 +41,9 @@ extern "C" int place(int token, int total, int W, int S) {
   const TokenPlace p = token_place(token, total, W, S);
   return p.full ? -1 - p.row : p.row;
 }
-extern "C" void chunks(int total, int W, int S, int n_splits, int *out) {
-  const Chunks c = chunks_of(total, W, S, n_splits);
+extern "C" int chunk_size(long long work, long long extra, int heads, int groups) { return chunk_for(work, extra, heads, groups); }
+extern "C" void chunks(int total, int W, int S, int chunk, int *out) {
+  const Chunks c = chunks_of(total, W, S, chunk);
   out[0] = c.n_kept; out[1] = c.n_win; out[2] = c.nq; out[3] = c.rows; out[4] = c.packed; out[5] = c.chunk;
 }
 extern "C" int page_ok(int x, int stride, int id, int n_pages) { return page_known(x, stride) && page_valid(id, n_pages); }
@@ -110,12 +111,11 @@ def test_units_of_sequences_do_not_overlap(plan, W, S):
         row0 = np.concatenate([[0], np.cumsum(news)])
         for i, n in enumerate(news):
             extra = int(rng.choice([0, 1, W - 1, W, 2 * W + 3]))
-            heads = int(rng.choice([1, 3, 8, 16]))
             most = {0: plan.append_units(n + extra, n, W, S),
-                    1: max(plan.fours_to_read(extra, n, S), plan.fours_to_read(0, n, S)), 2: n, 3: -(-n * heads // 16)}
+                    1: max(plan.fours_to_read(extra, n, S), plan.fours_to_read(0, n, S)), 2: n}
             for kind, units in most.items():
-                gap = plan.start_of(kind, heads, int(row0[i + 1]), i + 1) - plan.start_of(kind, heads, int(row0[i]), i)
-                assert units <= gap, (kind, n, extra, heads)
+                gap = plan.start_of(kind, int(row0[i + 1]), i + 1) - plan.start_of(kind, int(row0[i]), i)
+                assert units <= gap, (kind, n, extra)
 
 
 def test_read_covers_its_tokens_once(plan):
@@ -135,12 +135,38 @@ def test_chunks_cover_all_rows(plan):
     out = np.zeros(6, np.int32)
     for total in [1, 2, 127, 128, 129, 133, 134, 384, 385, 700, 4000, 131072, 2 ** 24 + 7, 2 ** 31 - 65]:
         for W, S in [(1, 0), (128, 0), (128, 5), (600, 1000), (1 << 20, 1 << 20)]:
-            for splits in [1, 2, 3, 7, 64, 128]:
-                plan.chunks(total, W, S, splits, out.ctypes.data_as(C.c_void_p))
+            for least in [256, 384, 4096, 2 ** 30]:
+                plan.chunks(total, W, S, least, out.ctypes.data_as(C.c_void_p))
                 kept, win, nq, rows, packed, chunk = (int(x) for x in out)
                 assert win == min(total, W) and kept == min(total - win, S) and kept + win + nq == total
-                assert rows == -(-(kept + win) // 512) and packed == -(-nq // chunk) <= splits
-                assert chunk % 128 == 0 and chunk >= 256
+                assert rows == -(-(kept + win) // 512) and packed == -(-nq // chunk) <= 128
+                assert chunk % 128 == 0 and chunk >= least
+
+
+@pytest.mark.parametrize("groups", [36, 512, 768])
+def test_units_fill_rounds_of_the_workgroups(plan, groups):
+    """The chunk size that the device finds: the batch's units fit whole rounds over the workgroups."""
+    rng = np.random.default_rng(groups)
+    out = np.zeros(6, np.int32)
+    plan.chunk_size.argtypes = [C.c_longlong, C.c_longlong, C.c_int, C.c_int]
+    for trial in range(300):
+        heads, W, S = int(rng.choice([1, 4, 8, 32])), int(rng.choice([1, 128, 700])), int(rng.choice([0, 5]))
+        lens = [int(10 ** rng.uniform(0, rng.uniform(1, 5.5))) for _ in range(rng.integers(1, 80))]
+        blocks = [int(rng.choice([0, 1, 1, 1, 4])) for _ in lens]
+
+        def chunks(total, least):
+            plan.chunks(total, W, S, least, out.ctypes.data_as(C.c_void_p))
+            return [int(x) for x in out]
+        got = [chunks(t, 256) for t in lens]
+        work = sum(b * c[2] for b, c in zip(blocks, got))
+        extra = sum(b * (c[3] + (c[2] > 0)) for b, c in zip(blocks, got))
+        size = plan.chunk_size(work, extra, heads, groups)
+        assert size % 128 == 0 and size >= 256
+        rounds = max(work * heads // (4096 * groups) + 1, -(-2 * extra * heads // groups))
+        units = heads * sum(b * (c[3] + c[4]) for b, c in zip(blocks, [chunks(t, size) for t in lens]))
+        assert units <= max(rounds, 1) * groups
+    assert plan.chunk_size(0, 0, 8, groups) == 256
+    assert plan.chunk_size(2 ** 31 * 2 ** 20, 2 ** 40, 65535, groups) >= 256
 
 
 def test_append_plan_at_the_longest_sequence(plan):
