@@ -13,7 +13,8 @@ namespace skvq {
 
 // Everything a kernel of the paged cache needs to find its data; passed by value.
 struct PagedLayout {
-  int Hq, Hk, R;  // R = Hq / Hk
+  int Hq, Hk, R;      // R = Hq / Hk
+  unsigned recip_R;   // recip_of(R)
   int G, NG;
   int W, S;
   int meta_fmt, meta_size;  // skvq_meta_format, bytes of a scale or zero
@@ -27,8 +28,8 @@ struct PagedLayout {
   void *k_rows, *v_rows;
   float *workspace;
   // device constants: channel of key code e of a row's dword m, at [head][8 m + e]; of value code n of piece
-  // m, at [head][8 m + n]
-  const uint8_t *k_channel, *v_channel;
+  // m, at [head][8 m + n]; and the place 8 m + e of a key channel
+  const uint8_t *k_channel, *v_channel, *k_place;
   const float *clip_k, *clip_v;  // [Hk][NG]
   int *errors;                   // SKVQ_PAGED_BAD_*
 };

@@ -22,7 +22,7 @@ struct skvq_paged {
   int device = 0;
   int n_cus = 256;
   int max_tokens = 0;
-  void *dev_consts = nullptr;  // k_channel, v_channel, clip_k, clip_v, errors
+  void *dev_consts = nullptr;  // k_channel, v_channel, k_place, clip_k, clip_v, errors
   char last_error[256] = "";
 };
 
@@ -231,6 +231,7 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
   L.Hq = cfg->n_q_heads;
   L.Hk = cfg->n_kv_heads;
   L.R = L.Hq / L.Hk;
+  L.recip_R = recip_of(L.R);
   L.G = cfg->group_size;
   L.NG = kD / L.G;
   L.W = cfg->window;
@@ -255,7 +256,7 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
   c->max_tokens = cfg->max_tokens;
 
   const size_t n_ch = (size_t)L.Hk * kD, n_clip = (size_t)L.Hk * L.NG;
-  const size_t off_v = n_ch, off_ck = 2 * n_ch, off_cv = off_ck + n_clip * 4, off_err = off_cv + n_clip * 4, total = off_err + 4;
+  const size_t off_v = n_ch, off_p = 2 * n_ch, off_ck = 3 * n_ch, off_cv = off_ck + n_clip * 4, off_err = off_cv + n_clip * 4, total = off_err + 4;
   std::unique_ptr<uint8_t[]> host(new (std::nothrow) uint8_t[total]());
   if (!host) return SKVQ_ERR_HIP;
   for (int h = 0; h < L.Hk; ++h)
@@ -263,6 +264,7 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
       for (int e = 0; e < 8; ++e) {
         const size_t at = (size_t)h * kD + 8 * m + e;
         host[at] = (uint8_t)cfg->perm_k[(size_t)h * kD + 32 * (m & 3) + 8 * (m >> 2) + e];
+        host[off_p + (size_t)h * kD + host[at]] = (uint8_t)(8 * m + e);
         host[off_v + at] = (uint8_t)cfg->perm_v[(size_t)h * kD + 16 * e + m];
       }
   std::memcpy(&host[off_ck], cfg->clip_k, n_clip * 4);
@@ -276,6 +278,7 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
   uint8_t *d = (uint8_t *)c->dev_consts;
   L.k_channel = d;
   L.v_channel = d + off_v;
+  L.k_place = d + off_p;
   L.clip_k = (const float *)(d + off_ck);
   L.clip_v = (const float *)(d + off_cv);
   L.errors = (int *)(d + off_err);
@@ -329,6 +332,7 @@ int skvq_paged_attention(skvq_paged *c, const skvq_batch *batch, const void *q, 
   if (rc != SKVQ_OK) return rc;
   if (batch->n_tokens > c->max_tokens) return SKVQ_ERR_INVALID_ARG;
   if (empty) return SKVQ_OK;
+  if ((long long)batch->n_tokens * c->L.R >= 1 << 27) return SKVQ_ERR_UNSUPPORTED;  // (query rows: see quotient)
   if (!rows_ok(q, q_stride, c->L.Hq) || (!out && !out_f32) || (out && !rows_ok(out, out_stride, c->L.Hq)) || !aligned(out_f32))
     return SKVQ_ERR_INVALID_ARG;
   OnDevice on(c->device);

@@ -12,12 +12,12 @@
 //   values  O^T[position][row] += V^T P^T, eight of the same instruction.  P^T is in the B operand's layout as it
 //           leaves S^T (lane: row lane % 16, tokens 4 (lane / 16) + 0..3 of both blocks), and a lane's 16 bytes of
 //           four value rows are the A operand's tokens of eight positions: nothing crosses lanes in the loop.
-// The (scale, zero) pairs of a lane's four tokens sit in the lanes of its row of 16, one pair each (token x / NG, group
-// x % NG in lane x): one load and one conversion per lane and block, and every use reads them by a lane broadcast that
-// is part of the instruction.
+// The (scale, zero) pairs of a lane's eight tokens, of keys and values, sit in the lanes of its row of 16 (PairSlot): one
+// load, conversion and logarithm per tile and group, and every use reads them by a lane broadcast that is part of the
+// instruction.
 //
-// The weight that multiplies a code is weight * scale: the reference counts log2 of the token's largest scale in,
-// so that this product, rounded to fp16 (half a step of 2^-10; a second part as in the fixed cache's kernel would refine
+// The weight that multiplies a code is weight * scale: the reference counts log2 of the largest scale at hand in, so
+// that this product, rounded to fp16 (half a step of 2^-10; a second part as in the fixed cache's kernel would refine
 // what 16-bit outputs do not show), stays within fp16's normal numbers near the largest contributions.  The middle code
 // goes into the zero and the rounded weights' own sum (one more matrix instruction, against ones) is taken off as often:
 // only a code's distance from the middle feels the rounding (error of a flat average of 32k tokens against 64 bits,
@@ -72,6 +72,17 @@ __device__ __forceinline__ float of_lane(float v) {
   return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + X, 0xF, 0xF, true));
 }
 
+// The largest of the row's 16 lanes, in all of them.
+__device__ __forceinline__ float row_max(float v) {
+  auto with = [](float x, auto ctrl) {
+    return fmaxf(x, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)));
+  };
+  v = with(v, std::integral_constant<int, 0xB1>{});   // lanes ^ 1, ^ 2, then mirror images of 8 and of 16
+  v = with(v, std::integral_constant<int, 0x4E>{});
+  v = with(v, std::integral_constant<int, 0x141>{});
+  return with(v, std::integral_constant<int, 0x140>{});
+}
+
 // One (scale, zero) pair as it comes from memory.
 template <int FMT>
 struct PairWord {
@@ -92,10 +103,22 @@ struct PairWord {
 };
 
 // A tile's packed data as a lane holds it.
-template <int FMT>
+template <int NG, int FMT>
 struct Tile {
   uint4_t k[2], v[2];
-  PairWord<FMT> km[2], vm[2];
+  PairWord<FMT> pairs[NG];
+};
+
+// Which pair lane c of a row of 16 holds in pairs[q]: 16 NG pairs in the order [keys, values][block][token of four][group].
+template <int NG>
+struct PairSlot {
+  int values, block, token, group;
+  __device__ __forceinline__ PairSlot(int q, int c) {
+    const int x = 16 * q + c;
+    values = x / (8 * NG), block = x / (4 * NG) % 2, token = x / NG % 4, group = x % NG;
+  }
+  static constexpr int load_of(int values, int block, int token, int group) { return ((values * 2 + block) * 4 + token) * NG / 16 + 0 * group; }
+  static constexpr int lane_of(int values, int block, int token, int group) { return (((values * 2 + block) * 4 + token) * NG + group) % 16; }
 };
 
 struct Out {
@@ -106,98 +129,120 @@ struct Out {
 
 // A unit's rows: up to 16 (query token, query head) rows of a kv head of one sequence.
 struct RowBlock {
-  int i;          // sequence
+  int i;      // sequence
   Sequence s;
-  int first;      // first of its rows, of n_new * R
-  int count;      // rows here
+  int first;  // first of its rows, of n_new * R
+  int count;  // rows here
 };
-// the query row's place in [n_tokens][Hq]
-__device__ __forceinline__ long long query_row(const PagedLayout &L, const RowBlock &x, int h, int row) {
-  const int y = x.first + row, j = y / L.R;
-  return (long long)(x.s.row0 + j) * L.Hq + h * L.R + (y - j * L.R);
+// Row y of the unit: its query token's row of the token arrays, its query head.
+struct QueryRow {
+  int token, head;
+};
+__device__ __forceinline__ QueryRow query_row(const PagedLayout &L, const RowBlock &x, int h, int row) {
+  const int y = x.first + row, j = quotient(y, L.recip_R);
+  return QueryRow{x.s.row0 + j, h * L.R + y - j * L.R};
 }
 
 template <class T>
-__device__ __forceinline__ void store_out(const PagedLayout &L, const Out &o, long long qrow, int channel, float x) {
-  if (o.out) {
-    const long long token = qrow / L.Hq, head = qrow - token * L.Hq;
-    reinterpret_cast<T *>(o.out)[token * o.stride + head * kD + channel] = (T)x;
-  }
-  if (o.f32) o.f32[qrow * kD + channel] = x;
+__device__ __forceinline__ void store_out(const PagedLayout &L, const Out &o, const QueryRow &q, int channel, float x) {
+  if (o.out) reinterpret_cast<T *>(o.out)[q.token * o.stride + q.head * kD + channel] = (T)x;
+  if (o.f32) o.f32[((long long)q.token * L.Hq + q.head) * kD + channel] = x;
 }
 
-// What a workgroup needs to know of the batch: the chunk size, and the units per kv head.  (Units are counted in 32 bits:
-// the host refuses a call that could have more.)
-struct BatchPlan {
-  int chunk, units;
-};
-// A sequence's blocks of 16 rows (none where its counts are bad) and its chunks.
-__device__ __forceinline__ int blocks_of(const PagedLayout &L, const Sequence &s) {
-  return s.counts_ok ? (int)(((long long)s.n_new * L.R + 15) >> 4) : 0;
-}
-__device__ __forceinline__ Chunks chunks_of_sequence(const PagedLayout &L, const Sequence &s, int chunk) {
-  return chunks_of(s.counts_ok ? s.total : 1, L.W, L.S, chunk);
+// Sum over the lanes up to this one, by moves within the register file (a shuffle goes through LDS).
+template <class V>
+__device__ __forceinline__ V lanes_up_to(V x) {
+  auto moved = [](V v, auto ctrl, auto rows) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+  };
+  typedef std::integral_constant<int, 0xF> all;
+  x += moved(x, std::integral_constant<int, 0x111>{}, all{});  // one lane up within the row of 16; 2, 4, 8
+  x += moved(x, std::integral_constant<int, 0x112>{}, all{});
+  x += moved(x, std::integral_constant<int, 0x114>{}, all{});
+  x += moved(x, std::integral_constant<int, 0x118>{}, all{});
+  x += moved(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});  // the last lane of rows 0 and 2 to the next rows
+  x += moved(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});  // lane 31 to the upper half
+  return x;
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long wave_sum(long long x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return (long long)(((unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32) | (unsigned)uniform((int)x));
+template <class V>
+__device__ __forceinline__ V last_lane(V x) {
+  return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-__device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const PagedBatch &b, int groups) {
+
+// A sequence of the batch with its chunks, and `blocks` blocks of 16 query rows (none where its counts are bad).
+struct Member {
+  Sequence s;
+  Chunks c;
+  int blocks;
+};
+__device__ __forceinline__ Member member_in_lane(const PagedLayout &L, const PagedBatch &b, int i, int chunk) {
+  Member m;
+  m.s = sequence_of(b, L, i < b.n_seqs ? i : b.n_seqs - 1);
+  m.blocks = i < b.n_seqs && m.s.counts_ok ? (m.s.n_new * L.R + 15) >> 4 : 0;
+  if (i >= b.n_seqs) m.s.counts_ok = true;
+  m.c = chunks_of(m.s.counts_ok ? m.s.total : 1, L.W, L.S, chunk);
+  return m;
+}
+// What a workgroup needs to know of the batch.  (Units are counted in 32 bits: the host refuses a call that could have
+// more.)  The first 64 sequences are kept in LDS, written by the first wavefront.
+struct BatchPlan {
+  int chunk, units;  // chunk size; units per kv head
+  int upto;          // units of the sequences up to number `lane`
+};
+__device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const PagedBatch &b, int groups, Member (&members)[64]) {
   const int lane = threadIdx.x & 63;
-  long long work = 0, extra = 0;
-  bool bad = false;
-  for (int i = lane; i < b.n_seqs; i += 64) {
-    const Sequence s = sequence_of(b, L, i);
-    bad = bad || !s.counts_ok;
-    const int blocks = blocks_of(L, s);
-    const Chunks c = chunks_of_sequence(L, s, kPagedMinChunk);
-    work += (long long)blocks * c.nq;
-    extra += (long long)blocks * (c.rows + (c.nq > 0));
-  }
-  if (bad && blockIdx.x == 0) atomicOr(L.errors, SKVQ_PAGED_BAD_COUNTS);
   BatchPlan p;
-  p.chunk = chunk_for(wave_sum(work), wave_sum(extra), L.Hk, groups);
-  int units = 0;
-  for (int i = lane; i < b.n_seqs; i += 64) {
-    const Sequence s = sequence_of(b, L, i);
-    const Chunks c = chunks_of_sequence(L, s, p.chunk);
-    units += blocks_of(L, s) * (c.rows + c.packed);
+  Member mine = member_in_lane(L, b, lane, kPagedMinChunk);
+  float work = 0.0f, extra = 0.0f;
+  bool bad = false;
+  Member m = mine;
+  for (int i0 = 0;;) {
+    bad = bad || !m.s.counts_ok;
+    work += (float)m.blocks * m.c.nq;
+    extra += (float)m.blocks * (m.c.rows + (m.c.nq > 0));
+    if ((i0 += 64) >= b.n_seqs) break;
+    m = member_in_lane(L, b, i0 + lane, kPagedMinChunk);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) units += __shfl_xor(units, d);
-  p.units = uniform(units);
+  if (bad && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(L.errors, SKVQ_PAGED_BAD_COUNTS);
+  p.chunk = uniform(chunk_for(last_lane(lanes_up_to(work)), last_lane(lanes_up_to(extra)), groups));
+  if (p.chunk != kPagedMinChunk) mine.c = chunks_of(mine.s.counts_ok ? mine.s.total : 1, L.W, L.S, p.chunk);
+  if (threadIdx.x < 64) members[lane] = mine;
+  p.upto = lanes_up_to(mine.blocks * (mine.c.rows + mine.c.packed));
+  p.units = last_lane(p.upto);
+  for (int i0 = 64; i0 < b.n_seqs; i0 += 64) {
+    m = member_in_lane(L, b, i0 + lane, p.chunk);
+    p.units += last_lane(lanes_up_to(m.blocks * (m.c.rows + m.c.packed)));
+  }
   return p;
 }
-// The unit's sequence, rows and chunk.  A chunk's row blocks are neighbours: they read the same rows.
-__device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, int unit, int &chunk) {
+// The unit's sequence with its chunks, its rows, its chunk.  A chunk's row blocks are neighbours: they read the same rows.
+__device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, const Member (&members)[64],
+                                              int unit, Chunks &c, int &chunk) {
   const int lane = threadIdx.x & 63;
   RowBlock x;
-  int rest = unit;
-  for (int i0 = 0;; i0 += 64) {
-    const int i = i0 + lane < b.n_seqs ? i0 + lane : b.n_seqs - 1;
-    const Sequence s = sequence_of(b, L, i);
-    const Chunks c = chunks_of_sequence(L, s, p.chunk);
-    int upto = i0 + lane < b.n_seqs ? blocks_of(L, s) * (c.rows + c.packed) : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(upto, d);
-      upto += lane >= d ? y : 0;
-    }
-    const unsigned long long behind = __ballot(upto > rest);  // (some lane, sooner or later: unit < p.units)
-    if (behind || i0 + 64 >= b.n_seqs) {
-      const int k = uniform(behind ? __ffsll(behind) - 1 : 63);
-      if (k > 0) rest -= __builtin_amdgcn_readlane(upto, k - 1);
-      x.i = i0 + k < b.n_seqs ? i0 + k : b.n_seqs - 1;
-      break;
-    }
-    rest -= __builtin_amdgcn_readlane(upto, 63);
+  int i0 = 0, upto = p.upto;
+  while (last_lane(upto) <= unit && i0 + 64 < b.n_seqs) {  // (unit < p.units)
+    unit -= last_lane(upto);
+    i0 += 64;
+    const Member m = member_in_lane(L, b, i0 + lane, p.chunk);
+    upto = lanes_up_to(m.blocks * (m.c.rows + m.c.packed));
   }
-  x.s = sequence_of(b, L, x.i);
-  const int blocks = blocks_of(L, x.s);
-  chunk = blocks > 1 ? rest / blocks : rest;
-  x.first = blocks > 1 ? 16 * (rest % blocks) : 0;
+  const unsigned long long behind = __ballot(upto > unit);
+  const int k = uniform(behind ? __ffsll(behind) - 1 : 63);
+  if (k > 0) unit -= __builtin_amdgcn_readlane(upto, k - 1);
+  x.i = i0 + k < b.n_seqs ? i0 + k : b.n_seqs - 1;
+  const Member m = i0 ? member_in_lane(L, b, x.i, p.chunk) : members[k];  // (the same in every lane)
+  x.s = Sequence{uniform(m.s.row0), uniform(m.s.n_new), uniform(m.s.total), uniform(m.s.slot), true, false};
+  x.s.slot_ok = x.s.slot >= 0 && x.s.slot < L.max_seqs;
+  c = Chunks{uniform(m.c.n_kept), uniform(m.c.n_win), uniform(m.c.nq), uniform(m.c.rows), uniform(m.c.packed), uniform(m.c.chunk)};
+  const int blocks = uniform(m.blocks);
+  chunk = unit;
+  x.first = 0;
+  if (blocks > 1) {
+    chunk = unit / blocks;
+    x.first = 16 * (unit - chunk * blocks);
+  }
   const int left = x.s.n_new * L.R - x.first;
   x.count = left < 16 ? left : 16;
   return x;
@@ -242,22 +287,32 @@ struct State {
 // behind what some query sees.  left: rows of the tile before the end; seen: before the last one that the lane's row
 // sees.  alpha: on the scores, with the code's unit.
 template <int NG, int FMT, bool MASKED>
-__device__ __forceinline__ void take_tile(State<NG> &st, const Tile<FMT> &t, const half8_t (&qb)[4], const float (&qs)[NG], float alpha,
+__device__ __forceinline__ void take_tile(State<NG> &st, const Tile<NG, FMT> &t, const half8_t (&qb)[4], const float (&qs)[NG], float alpha,
                                           int left, int seen, int g, int c) {
-  float ks[2], kz[2], vs[2], vz[2], lg[2];
+  typedef PairSlot<NG> Slot;
+  // scale (of keys: times alpha) and zero (of values: with the middle code in it); the logarithm of the largest scale of
+  // the lane's row of values
+  float scale[NG], zero[NG], most = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float2 k = t.km[i].value(), v = t.vm[i].value();
-    const bool there = !MASKED || 16 * i + 4 * g + (c % (4 * NG)) / NG < left;
-    ks[i] = there ? k.x * alpha : 0.0f;
-    kz[i] = there ? k.y : 0.0f;
-    vs[i] = there ? v.x : 0.0f;
-    vz[i] = there ? fmaf(v.x, kMidCode, v.y) : 0.0f;
-    float most = vs[i];
-    if (NG >= 2) most = fmaxf(most, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(most), 0xB1, 0xF, 0xF, true)));
-    if (NG == 4) most = fmaxf(most, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(most), 0x4E, 0xF, 0xF, true)));
-    lg[i] = fmaxf(__builtin_amdgcn_logf(most), kLowestLog);
+  for (int q = 0; q < NG; ++q) {
+    const Slot slot(q, c);
+    const float2 pair = t.pairs[q].value();
+    const bool there = !MASKED || 16 * slot.block + 4 * g + slot.token < left;
+    const float x = there ? pair.x : 0.0f, z = there ? pair.y : 0.0f;
+    if (NG == 1) {  // (keys and values side by side)
+      scale[q] = x * (slot.values ? 1.0f : alpha);
+      zero[q] = fmaf(x, slot.values ? kMidCode : 0.0f, z);
+      most = slot.values ? x : 0.0f;
+    } else if (q < NG / 2) {
+      scale[q] = x * alpha;
+      zero[q] = z;
+    } else {
+      scale[q] = x;
+      zero[q] = fmaf(x, kMidCode, z);
+      most = fmaxf(most, x);
+    }
   }
+  most = row_max(most);
   float s[8], top = -INFINITY;
   const unsigned mask = 0x00f000f0u;
   unrolled<0, 2>([&](auto I) {
@@ -274,26 +329,25 @@ __device__ __forceinline__ void take_tile(State<NG> &st, const Tile<FMT> &t, con
       constexpr int r = R();
       float x = 0.0f;
       unrolled<0, NG>([&](auto N) {
-        constexpr int n = N();
-        x = n == 0 ? of_lane<r * NG>(kz[i]) * qs[0] : fmaf(of_lane<r * NG + n>(kz[i]), qs[n], x);
-        x = fmaf(of_lane<r * NG + n>(ks[i]), acc[n][r], x);
+        constexpr int n = N(), q = Slot::load_of(0, i, r, n), lane = Slot::lane_of(0, i, r, n);
+        x = n == 0 ? of_lane<lane>(zero[q]) * qs[0] : fmaf(of_lane<lane>(zero[q]), qs[n], x);
+        x = fmaf(of_lane<lane>(scale[q]), acc[n][r], x);
       });
-      const float u = of_lane<r * NG>(lg[i]) + x;
       const bool there = !MASKED || 16 * i + 4 * g + r < min(left, seen);
       s[4 * i + r] = there ? x : -INFINITY;
-      top = fmaxf(top, there ? u : -INFINITY);
+      top = fmaxf(top, s[4 * i + r]);
     });
   });
-  st.refer(top);
+  st.refer(top + fmaxf(__builtin_amdgcn_logf(most), kLowestLog));
   half8_t pb[NG];
   unrolled<0, 8>([&](auto I) {
     constexpr int i = I() / 4, r = I() % 4;
     const float p = __builtin_amdgcn_exp2f(s[I()] - st.m);
     st.l += p;
     unrolled<0, NG>([&](auto N) {
-      constexpr int n = N();
-      st.z[n] = fmaf(of_lane<r * NG + n>(vz[i]), p, st.z[n]);
-      pb[n][I()] = (_Float16)(of_lane<r * NG + n>(vs[i]) * p);
+      constexpr int n = N(), q = Slot::load_of(1, i, r, n), lane = Slot::lane_of(1, i, r, n);
+      st.z[n] = fmaf(of_lane<lane>(zero[q]), p, st.z[n]);
+      pb[n][I()] = (_Float16)(of_lane<lane>(scale[q]) * p);
     });
   });
   const half8_t one = as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
@@ -314,114 +368,139 @@ __device__ __forceinline__ void take_tile(State<NG> &st, const Tile<FMT> &t, con
 template <class T>
 struct Lds {
   union alignas(16) {
-    T q[16][kD + 8];
+    T q[16][kD + 8];  // the queries; for packed rows a head's channels in the order of the key codes
     float acc[kWaves][16][kRowStride];
   };
   float m[kWaves][16], l[kWaves][16];
   int bad;
+  Member members[64];
 };
 
-// The wavefront's share of a chunk of packed rows.
-template <class T, int NG, int FMT>
-__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T> &lds, const RowBlock &x, const Chunks &ch,
-                                            int chunk, int h, State<NG> &st, bool &bad) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int last = x.s.total - x.s.n_new + (x.first + (c < x.count ? c : x.count - 1)) / L.R;  // lane's row: the last token it sees
-  // B operand: row c's queries at the reordered positions of key dword 4g + j, as fp16 numbers.  bf16 queries are
-  // brought to fp16's range by one power of two: what that makes subnormal is 2^-25 of the largest.
-  half8_t qb[4];
-  float qs[NG], scale = L.sm_scale * kLog2e, alpha = scale * kCodeUnit;
-  {
-    float v[4][8], most = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned long long at = *reinterpret_cast<const unsigned long long *>(L.k_channel + h * kD + 8 * (4 * g + j));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[j][e] = (float)lds.q[c][(at >> (8 * e)) & 0xffu];
-        most = fmaxf(most, fabsf(v[j][e]));
-      }
-    }
-    float to_half = 1.0f;
-    if constexpr (!__is_same(T, _Float16)) {
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-      const int exponent = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;  // most in [2^(e-1), 2^e)
-      to_half = __builtin_amdgcn_ldexpf(1.0f, 14 - exponent < 126 ? 14 - exponent : 126);
-      alpha /= to_half;
-    }
-#pragma unroll
-    for (int t = 0; t < NG; ++t) qs[t] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        qs[j * NG / 4] += v[j][e];
-        qb[j][e] = (_Float16)(v[j][e] * to_half);
-      }
-#pragma unroll
-    for (int t = 0; t < NG; ++t) {
-      qs[t] += __shfl_xor(qs[t], 16);
-      qs[t] += __shfl_xor(qs[t], 32);
-      qs[t] *= scale;
+// Pages of the wavefront's tiles k0 .. k0 + 31 of a chunk [begin, end) of packed rows, two blocks of 16 tokens each: lane
+// 2k + i holds tile k0 + k's block i.
+__device__ __forceinline__ int pages_of_tiles(const PagedLayout &L, const PagedBatch &b, int seq, int begin, int end, int k0, bool &bad) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int te = begin + kTile * (wave + kWaves * (k0 + (lane >> 1))) + 16 * (lane & 1);
+  int id = 0;
+  if (te < end) {
+    const int at = te >> L.page_log2;
+    id = page_known(at, b.table_stride) ? b.table[(long long)seq * b.table_stride + at] : -1;
+    if (!page_valid(id, L.n_pages)) {
+      bad = true;
+      id = 0;
     }
   }
+  return id;
+}
+
+// The wavefront's share of a chunk of packed rows.  ids: pages_of_tiles of its first tiles.
+template <class T, int NG, int FMT>
+__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T> &lds, const RowBlock &x, const Chunks &ch,
+                                            int chunk, int h, int ids, State<NG> &st, bool &bad) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+  const int last = x.s.total - x.s.n_new + (x.first + (c < x.count ? c : x.count - 1)) / L.R;  // lane's row: the last token it sees
   const int seen = last + 1 - L.S;  // packed rows that the lane's row sees; all of them see the first row's
   const int begin = chunk * ch.chunk, end = min(ch.nq, begin + ch.chunk);
   const int all_see = min(end, x.s.total - x.s.n_new + x.first / L.R + 1 - L.S);
   const int n_tiles = (end - begin + kTile - 1) / kTile, mine = n_tiles > wave ? (n_tiles - wave + kWaves - 1) / kWaves : 0;
   const uint8_t *head_part = L.pages + (long long)h * L.part_bytes;
   const long long page_stride = (long long)L.Hk * L.part_bytes;
-  const int *table = b.table + (long long)x.i * b.table_stride;
   constexpr int kPair = PairWord<FMT>::kSize;
   const unsigned k_lane = c * (kD / 2) + 16 * g, v_lane = L.v_at + 256 * g + 16 * c;
-  const unsigned m_lane = kPair * (4 * NG * g + c % (4 * NG));
-  // Pages of the wavefront's next 32 tiles, two blocks of 16 tokens each: lane 2k + i holds tile k's block i.
-  int ids = 0;
-  auto look_up = [&](int k0) {
-    const int te = begin + kTile * (wave + kWaves * (k0 + (lane >> 1))) + 16 * (lane & 1);
-    ids = 0;
-    if (te < end) {
-      const int at = te >> L.page_log2;
-      ids = page_known(at, b.table_stride) ? table[at] : -1;
-      if (!page_valid(ids, L.n_pages)) {
-        bad = true;
-        ids = 0;
-      }
-    }
-  };
-  auto load = [&](Tile<FMT> &t, int k) {  // the wavefront's k-th tile, if there is one (blocks past the end: of page 0)
-    if (k >= mine) return;
-    if ((k & 31) == 0) look_up(k);
+  unsigned pair_lane[NG];
+  bool pair_block[NG];
+#pragma unroll
+  for (int q = 0; q < NG; ++q) {
+    const PairSlot<NG> slot(q, c);
+    pair_lane[q] = (slot.values ? L.vm_at : L.km_at) + kPair * ((4 * g + slot.token) * NG + slot.group);
+    pair_block[q] = slot.block;
+  }
+  // The wavefront's k-th tile, of those that `ids` holds from the k0-th on (blocks past the end: of page 0).
+  // Codes are read once per row block, by instructions that take whole lines: streaming loads.
+  auto load = [&](Tile<NG, FMT> &t, int k, int k0) {
+    const uint8_t *part[2];
+    unsigned place[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int id = __builtin_amdgcn_readlane(ids, 2 * (k & 31) + i);
+      const int id = __builtin_amdgcn_readlane(ids, 2 * (k - k0) + i);
       const int te = begin + kTile * (wave + kWaves * k) + 16 * i;
-      const unsigned place = te & ((1 << L.page_log2) - 1);
-      const uint8_t *p = head_part + id * page_stride;
-      t.k[i] = *reinterpret_cast<const uint4_t *>(p + place * (kD / 2) + k_lane);
-      t.v[i] = *reinterpret_cast<const uint4_t *>(p + place * (kD / 2) + v_lane);
-      t.km[i].load(p + place * (NG * kPair) + L.km_at + m_lane);
-      t.vm[i].load(p + place * (NG * kPair) + L.vm_at + m_lane);
+      place[i] = te & ((1 << L.page_log2) - 1);
+      part[i] = head_part + id * page_stride;
+      const uint8_t *codes = part[i] + place[i] * (kD / 2);
+      t.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(codes + k_lane));
+      t.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(codes + v_lane));
+    }
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
+      const uint8_t *p0 = part[0] + place[0] * (NG * kPair), *p1 = part[1] + place[1] * (NG * kPair);
+      t.pairs[q].load((pair_block[q] ? p1 : p0) + pair_lane[q]);
     }
   };
-  // Whole tiles that every query sees, two buffers in turn; then the others (at the chunk's end).
+  Tile<NG, FMT> even, odd;
+  if (mine > 0) load(even, 0, 0);
+  // B operand: row c's queries at the reordered positions of key dword 4g + j, as fp16 numbers.  bf16 queries are
+  // brought to fp16's range by one power of two: what that makes subnormal is 2^-25 of the largest.
+  half8_t qb[4];
+  float qs[NG], scale = L.sm_scale * kLog2e, alpha = scale * kCodeUnit;
+  {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const t8 *>(&lds.q[c][8 * (4 * g + j)]);
+#pragma unroll
+    for (int n = 0; n < NG; ++n) qs[n] = 0.0f;
+    float to_half = 1.0f;
+    if constexpr (!__is_same(T, _Float16)) {
+      float most = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)v[j][e]));
+      most = row_max(most);
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const int exponent = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;  // most in [2^(e-1), 2^e)
+      to_half = __builtin_amdgcn_ldexpf(1.0f, 14 - exponent < 126 ? 14 - exponent : 126);
+      alpha /= to_half;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        qs[j * NG / 4] += (float)v[j][e];
+        if constexpr (__is_same(T, _Float16))
+          qb[j][e] = v[j][e];
+        else
+          qb[j][e] = (_Float16)((float)v[j][e] * to_half);
+      }
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      qs[n] += __shfl_xor(qs[n], 16);
+      qs[n] += __shfl_xor(qs[n], 32);
+      qs[n] *= scale;
+    }
+  }
+  // Whole tiles that every query sees, two buffers in turn; then the others (at the chunk's end).  The lanes hold the pages
+  // of 32 tiles, and the next tile is on its way while one is worked on (the last one's loads are repeated: no branch
+  // between loads and what they hide behind): 30 tiles a turn.
   const int whole_tiles = all_see > begin ? (all_see - begin) / kTile : 0;
   const int whole = whole_tiles > wave ? (whole_tiles - wave + kWaves - 1) / kWaves : 0;
-  Tile<FMT> even, odd;
-  load(even, 0);
-  int k = 0;
-  for (; k + 1 < whole; k += 2) {
-    load(odd, k + 1);
-    take_tile<NG, FMT, false>(st, even, qb, qs, alpha, 0, 0, g, c);
-    load(even, k + 2);
-    take_tile<NG, FMT, false>(st, odd, qb, qs, alpha, 0, 0, g, c);
-  }
-  for (; k < mine; ++k) {
-    const int te0 = begin + kTile * (wave + kWaves * k);
-    load(odd, k + 1);
-    take_tile<NG, FMT, true>(st, even, qb, qs, alpha, end - te0, seen - te0, g, c);
-    even = odd;
+  for (int k0 = 0; k0 < mine; k0 += 30) {
+    if (k0 > 0) ids = pages_of_tiles(L, b, x.i, begin, end, k0, bad);
+    const int stop = min(mine, k0 + 30);
+    int k = k0;
+    for (const int stop_whole = min(stop, whole); k + 1 < stop_whole; k += 2) {
+      load(odd, k + 1, k0);
+      take_tile<NG, FMT, false>(st, even, qb, qs, alpha, 0, 0, g, c);
+      load(even, min(k + 2, mine - 1), k0);
+      take_tile<NG, FMT, false>(st, odd, qb, qs, alpha, 0, 0, g, c);
+    }
+    for (; k < stop; ++k) {
+      const int te0 = begin + kTile * (wave + kWaves * k);
+      load(odd, min(k + 1, mine - 1), k0);
+      take_tile<NG, FMT, true>(st, even, qb, qs, alpha, end - te0, seen - te0, g, c);
+      even = odd;
+    }
   }
 }
 
@@ -498,31 +577,43 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
   typedef Piece<T, 8> P;
   __shared__ Lds<T> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const BatchPlan plan = plan_batch(L, b, gridDim.x);
-  for (int at = blockIdx.x; at < plan.units * L.Hk; at += gridDim.x) {
-    const int unit = at / L.Hk, h = at - unit * L.Hk;
+  const int h = blockIdx.x;  // (heads side by side: a head's units, row blocks of one chunk among them, share a chiplet's L2)
+  const unsigned long long places = *reinterpret_cast<const unsigned long long *>(L.k_place + h * kD + 8 * c);
+  const int p = threadIdx.x % kD, packed_channel = L.v_channel[h * kD + 8 * (p & 15) + (p >> 4)];  // of the output place it writes
+  const BatchPlan plan = plan_batch(L, b, gridDim.y, lds.members);
+  __syncthreads();
+  for (int unit = blockIdx.y; unit < plan.units; unit += gridDim.y) {
     int chunk;
-    const RowBlock x = find_unit(L, b, plan, unit, chunk);
-    const Chunks ch = chunks_of(x.s.total, L.W, L.S, plan.chunk);
+    Chunks ch;
+    const RowBlock x = find_unit(L, b, plan, lds.members, unit, ch, chunk);
     const bool packed = chunk >= ch.rows;
+    // the queries, sixteen threads a row, rows past the last one repeat it; the first pages meanwhile
+    static_assert(64 * kWaves == 16 * 16, "one piece of a row per thread");
+    const int query = threadIdx.x >> 4;
+    const QueryRow from = query_row(L, x, h, query < x.count ? query : x.count - 1);
+    const P mine = *reinterpret_cast<const P *>((const T *)q.p + from.token * q.stride + from.head * kD + 8 * c);
+    bool bad = false;
+    int ids = 0;
+    if (packed) {
+      const int begin = (chunk - ch.rows) * ch.chunk;
+      ids = pages_of_tiles(L, b, x.i, begin, min(ch.nq, begin + ch.chunk), 0, bad);
+    }
     __syncthreads();  // (the unit before has read its partials out of LDS)
     if (threadIdx.x == 0) {
       lds.bad = !x.s.slot_ok;
       if (!x.s.slot_ok) atomicOr(L.errors, SKVQ_PAGED_BAD_SLOT);
     }
-    // the queries, rows past the last one repeat it
-    for (int y = threadIdx.x; y < 16 * 16; y += 64 * kWaves) {
-      const int row = y >> 4, m = y & 15;
-      const long long qr = query_row(L, x, h, row < x.count ? row : x.count - 1);
-      const long long token = qr / L.Hq, head = qr - token * L.Hq;
-      *reinterpret_cast<P *>(&lds.q[row][8 * m]) = *reinterpret_cast<const P *>((const T *)q.p + token * q.stride + head * kD + 8 * m);
+    if (packed) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) lds.q[query][(places >> (8 * e)) & 0xffu] = mine[e];
+    } else {
+      *reinterpret_cast<P *>(&lds.q[query][8 * c]) = mine;
     }
     __syncthreads();
     State<NG> st;
     st.clear();
-    bool bad = false;
     if (packed)
-      take_packed<T, NG, FMT>(L, b, lds, x, ch, chunk - ch.rows, h, st, bad);
+      take_packed<T, NG, FMT>(L, b, lds, x, ch, chunk - ch.rows, h, ids, st, bad);
     else if (x.s.slot_ok)
       take_rows<T, NG>(L, lds, x, ch, chunk, h, st);
 
@@ -562,8 +653,8 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
     }
     __syncthreads();
     const int n_partials = ch.rows + ch.packed, most = kPagedMaxSplits + n_row_chunks;
-    for (int y = threadIdx.x; y < x.count * kD; y += 64 * kWaves) {
-      const int row = y / kD, p = y % kD;
+    const int channel = packed ? packed_channel : p;
+    for (int row = threadIdx.x / kD; row < x.count; row += 64 * kWaves / kD) {
       float acc = lds.acc[0][row][p], m = lds.m[0][row], l = 0.0f;
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) {
@@ -573,9 +664,8 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) l += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - m);
       if (lds.bad) l = NAN;
-      const int channel = packed ? L.v_channel[h * kD + 8 * (p & 15) + (p >> 4)] : p;
-      const long long qr = query_row(L, x, h, row);
-      float *to = L.workspace + qr * most * kPartialStride;
+      const QueryRow qr = query_row(L, x, h, row);
+      float *to = L.workspace + ((long long)qr.token * L.Hq + qr.head) * most * kPartialStride;
       if (n_partials == 1) {
         store_out<T>(L, out, qr, channel, acc / l);
       } else {
@@ -598,23 +688,22 @@ template <class T>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedLayout L, const PagedBatch b, const Out out, int n_row_chunks) {
   __shared__ float weight[kMergeThreads], red[2][kMergeThreads / 64];
   __shared__ float4_t parts[kMergeGroups][32];
-  const int token = blockIdx.x, tid = threadIdx.x;
-  const Sequence s = sequence_of(b, L, sequence_of_unit(b, token, kTokenDeal));
-  if (!s.counts_ok || token < s.row0 || token >= s.row0 + s.n_new) return;
-  const long long qr = (long long)token * L.Hq + blockIdx.y;
-  const float *from = L.workspace + qr * (kPagedMaxSplits + n_row_chunks) * kPartialStride;
-  const int n = (int)__float_as_uint(from[2]);
-  if (n <= 1) return;
+  const int token = blockIdx.x, tid = threadIdx.x, group = tid >> 5, t = tid & 31;
+  const QueryRow qr = {token, (int)blockIdx.y};
+  const float *from = L.workspace + ((long long)token * L.Hq + qr.head) * (kPagedMaxSplits + n_row_chunks) * kPartialStride;
   auto partial = [&](int i) { return from + (long long)i * kPartialStride; };
+  const int n = (int)__float_as_uint(from[2]);  // (anything where the token is of no sequence)
+  const Sequence s = sequence_of(b, L, sequence_of_unit(b, token, kTokenDeal));
+  if (!s.counts_ok || token < s.row0 || token >= s.row0 + s.n_new || n <= 1) return;
   float m = kNothing, l = 0.0f;
   float4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = 0; i0 < n; i0 += kMergeThreads) {  // (more than 256 only with windows of ten thousands of tokens)
-    const int here = min(kMergeThreads, n - i0), t = tid & 31;
-    const float mi = tid < here ? partial(i0 + tid)[0] : kNothing;
-    const float li = tid < here ? partial(i0 + tid)[1] : 0.0f;
-    float top = mi;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const int here = min(kMergeThreads, n - i0);
+    const float2 ml = tid < here ? *reinterpret_cast<const float2 *>(partial(i0 + tid)) : make_float2(kNothing, 0.0f);
+    const float mi = ml.x;
+    float top = row_max(mi);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
     if ((tid & 63) == 0) red[0][tid >> 6] = top;
     __syncthreads();
     top = m;
@@ -622,9 +711,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
     for (int w = 0; w < kMergeThreads / 64; ++w) top = fmaxf(top, red[0][w]);
     const float w = tid < here ? __builtin_amdgcn_exp2f(mi - top) : 0.0f, before = __builtin_amdgcn_exp2f(m - top);
     weight[tid] = w;
-    float sum = li * w;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    const float sum = last_lane(lanes_up_to(ml.y * w));
     if ((tid & 63) == 0) red[1][tid >> 6] = sum;
     __syncthreads();
     l *= before;
@@ -632,7 +719,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
     for (int w = 0; w < kMergeThreads / 64; ++w) l += red[1][w];
     acc *= before;
     m = top;
-    int i = tid >> 5;
+    int i = group;
     for (; i + 3 * kMergeGroups < here; i += 4 * kMergeGroups) {
       float4_t a[4];
 #pragma unroll
@@ -643,7 +730,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
     for (; i < here; i += kMergeGroups) acc += *reinterpret_cast<const float4_t *>(partial(i0 + i) + 4 + 4 * t) * weight[i];
     __syncthreads();
   }
-  parts[tid >> 5][tid & 31] = acc;
+  parts[group][t] = acc;
   __syncthreads();
   if (tid < kD) {
     float x = 0.0f;
@@ -655,11 +742,11 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
 
 template <class T, int NG>
 void launch_chunks(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
-  const dim3 threads(64 * kWaves);
+  const dim3 grid(L.Hk, groups), threads(64 * kWaves);
   switch (L.meta_fmt) {
-    case SKVQ_META_F32: paged_attention_kernel<T, NG, SKVQ_META_F32><<<groups, threads, 0, s>>>(L, b, q, out, row_chunks); break;
-    case SKVQ_META_F16: paged_attention_kernel<T, NG, SKVQ_META_F16><<<groups, threads, 0, s>>>(L, b, q, out, row_chunks); break;
-    default: paged_attention_kernel<T, NG, SKVQ_META_FP8_E4M3><<<groups, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    case SKVQ_META_F32: paged_attention_kernel<T, NG, SKVQ_META_F32><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    case SKVQ_META_F16: paged_attention_kernel<T, NG, SKVQ_META_F16><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    default: paged_attention_kernel<T, NG, SKVQ_META_FP8_E4M3><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
   }
 }
 
@@ -682,14 +769,14 @@ hipError_t launch_paged_attention(const PagedLayout &L, const skvq_batch &batch,
                                   float *out_f32, int n_cus, hipStream_t s) {
   const PagedBatch b = batch_of(batch);
   const int row_chunks = paged_row_chunks(L.W, L.S);
-  // Lengths are not known here: as many workgroups as the chip holds at once, unless there can be no more units than
-  // that (every row in a block of its own sequence, every sequence as long as the page table allows).
+  // Lengths are not known here: as many workgroups as the chip holds at once, over the kv heads, unless there can be no
+  // more units than that (every query token of a sequence of its own, as long as the page table allows).
   const long long rows = (long long)b.n_tokens * L.R, blocks = rows / 16 + (b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens);
   long long splits = ((long long)b.table_stride << L.page_log2) / kPagedMinChunk + 1;
   if (splits > kPagedMaxSplits) splits = kPagedMaxSplits;
-  const long long units = blocks * (row_chunks + splits) * L.Hk, most = (long long)groups_per_cu(L.NG) * n_cus;
-  if (units > 0x7fffffff - most) return hipErrorInvalidValue;  // (counted in 32 bits)
-  const unsigned groups = (unsigned)(units < most ? units : most);
+  const long long units = blocks * (row_chunks + splits), most = (long long)groups_per_cu(L.NG) * n_cus / L.Hk;
+  if (units > 1 << 30) return hipErrorInvalidValue;  // (counted in 32 bits)
+  const unsigned groups = (unsigned)(units < most ? units : most > 0 ? most : 1);
   const Out o{out, out_stride, out_f32};
   return L.dtype == SKVQ_DTYPE_BF16 ? launch_typed<__bf16>(L, b, q, o, row_chunks, groups, s)
                                     : launch_typed<_Float16>(L, b, q, o, row_chunks, groups, s);

@@ -87,20 +87,22 @@ constexpr int kPagedMaxSplits = 128;     // chunks of packed rows of a sequence
 constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
 constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
 constexpr int whole_steps(int rows) { return (rows / kPagedStep + (rows % kPagedStep > 0)) * kPagedStep; }
-// Lengths are known on the device only, so every workgroup of a launch of `groups` finds the batch's chunk size from two
-// sums over the batch, per kv head: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a
+// Lengths are known on the device only, so every workgroup, of `groups` per kv head, finds the batch's chunk size from two
+// sums over the batch: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a
 // chunk of full rows and a last, shorter chunk of packed ones per block).  The units fit `rounds` rounds over the
-// groups: as few as keep a chunk within 4096 rows, more where the extra units would fill half of them.
-constexpr int chunk_for(long long work, long long extra, int heads, int groups) {
-  work = (work < 1ll << 45 ? work : 1ll << 45) * heads;  // (beyond, a chunk is as long as it can be)
-  extra = (extra < 1ll << 40 ? extra : 1ll << 40) * heads;
-  long long rounds = work / (4096ll * groups) + 1;
-  const long long full = (2 * extra + groups - 1) / groups;
-  if (rounds < full) rounds = full;
-  const long long units = rounds * groups - extra, rows = (work + units - 1) / units;
-  const int chunk = whole_steps(rows < 0x40000000 ? (int)rows : 0x40000000);
+// groups of a head: as few as keep a chunk within 4096 rows, more where the extra units would fill half of them.
+// (Numbers of 24 bits do: the units are counted exactly from the chunk size, which is the same in every workgroup.)
+constexpr int chunk_for(float work, float extra, int groups) {
+  const float least = work / (4096.0f * groups), full = 2.0f * extra / groups;
+  const float most = least > full ? least : full;
+  const float rounds = (float)(int)(most < 1e6f ? most : 1e6f) + 1.0f;
+  const float rows = work / (rounds * groups - extra);  // (positive: rounds > full)
+  const int chunk = whole_steps(rows < 1e9f ? (int)rows + 1 : 1000000000);
   return chunk < kPagedMinChunk ? kPagedMinChunk : chunk;
 }
+// Quotient by a number of 1 .. 16 (recip_of it) of y < 2^27.
+constexpr unsigned recip_of(int divisor) { return ((1u << 31) + divisor - 1) / divisor; }
+constexpr int quotient(int y, unsigned recip) { return (int)(((unsigned long long)(2u * (unsigned)y) * recip) >> 32); }
 struct Chunks {
   int n_kept, n_win, nq;    // sink rows, ring rows, packed rows
   int rows, packed, chunk;  // chunks of full rows, of packed rows; packed rows per chunk

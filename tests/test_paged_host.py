@@ -41,7 +41,8 @@ extern "C" int place(int token, int total, int W, int S) {
   const TokenPlace p = token_place(token, total, W, S);
   return p.full ? -1 - p.row : p.row;
 }
-extern "C" int chunk_size(long long work, long long extra, int heads, int groups) { return chunk_for(work, extra, heads, groups); }
+extern "C" int chunk_size(float work, float extra, int groups) { return chunk_for(work, extra, groups); }
+extern "C" int divided(int y, int by) { return quotient(y, recip_of(by)); }
 extern "C" void chunks(int total, int W, int S, int chunk, int *out) {
   const Chunks c = chunks_of(total, W, S, chunk);
   out[0] = c.n_kept; out[1] = c.n_win; out[2] = c.nq; out[3] = c.rows; out[4] = c.packed; out[5] = c.chunk;
@@ -143,14 +144,14 @@ def test_chunks_cover_all_rows(plan):
                 assert chunk % 128 == 0 and chunk >= least
 
 
-@pytest.mark.parametrize("groups", [36, 512, 768])
+@pytest.mark.parametrize("groups", [1, 24, 96, 768])
 def test_units_fill_rounds_of_the_workgroups(plan, groups):
     """The chunk size that the device finds: the batch's units fit whole rounds over the workgroups."""
     rng = np.random.default_rng(groups)
     out = np.zeros(6, np.int32)
-    plan.chunk_size.argtypes = [C.c_longlong, C.c_longlong, C.c_int, C.c_int]
+    plan.chunk_size.argtypes = [C.c_float, C.c_float, C.c_int]
     for trial in range(300):
-        heads, W, S = int(rng.choice([1, 4, 8, 32])), int(rng.choice([1, 128, 700])), int(rng.choice([0, 5]))
+        W, S = int(rng.choice([1, 128, 700])), int(rng.choice([0, 5]))
         lens = [int(10 ** rng.uniform(0, rng.uniform(1, 5.5))) for _ in range(rng.integers(1, 80))]
         blocks = [int(rng.choice([0, 1, 1, 1, 4])) for _ in lens]
 
@@ -160,13 +161,19 @@ def test_units_fill_rounds_of_the_workgroups(plan, groups):
         got = [chunks(t, 256) for t in lens]
         work = sum(b * c[2] for b, c in zip(blocks, got))
         extra = sum(b * (c[3] + (c[2] > 0)) for b, c in zip(blocks, got))
-        size = plan.chunk_size(work, extra, heads, groups)
+        size = plan.chunk_size(work, extra, groups)
         assert size % 128 == 0 and size >= 256
-        rounds = max(work * heads // (4096 * groups) + 1, -(-2 * extra * heads // groups))
-        units = heads * sum(b * (c[3] + c[4]) for b, c in zip(blocks, [chunks(t, size) for t in lens]))
-        assert units <= max(rounds, 1) * groups
-    assert plan.chunk_size(0, 0, 8, groups) == 256
-    assert plan.chunk_size(2 ** 31 * 2 ** 20, 2 ** 40, 65535, groups) >= 256
+        rounds = max(work / (4096 * groups), 2 * extra / groups) * (1 + 1e-6) // 1 + 1
+        units = sum(b * (c[3] + c[4]) for b, c in zip(blocks, [chunks(t, size) for t in lens]))
+        assert units <= rounds * groups
+    assert plan.chunk_size(0, 0, groups) == 256
+    assert plan.chunk_size(2.0 ** 62, 2.0 ** 40, groups) >= 256
+
+
+def test_quotients(plan):
+    for by in range(1, 17):
+        for y in [0, 1, by - 1, by, by + 1, 12345, *range(2 ** 27 - 40, 2 ** 27), *(by * (2 ** 23 + k) - 1 for k in range(3))]:
+            assert plan.divided(y, by) == y // by
 
 
 def test_append_plan_at_the_longest_sequence(plan):
