@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -116,17 +117,17 @@ def lib() -> C.CDLL:
         L.skvq_rope_destroy.argtypes = [C.c_void_p]
         L.skvq_rope_destroy.restype = None
         L.skvq_rope_frequencies.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
-        L.skvq_rope_apply.argtypes = [C.c_void_p, C.POINTER(skvq_rope_tensor), C.c_int32, C.c_int32, C.c_int32, C.c_int64,
+        L.skvq_rope_apply.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64,
                                       C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p]
         L.skvq_paged_sizes.argtypes = [C.POINTER(skvq_paged_config), C.POINTER(C.c_size_t)]
         L.skvq_paged_validate_config.argtypes = [C.POINTER(skvq_paged_config)]
         L.skvq_paged_create.argtypes = [C.POINTER(skvq_paged_config), C.POINTER(skvq_paged_buffers), C.POINTER(C.c_void_p)]
         L.skvq_paged_destroy.argtypes = [C.c_void_p]
         L.skvq_paged_destroy.restype = None
-        L.skvq_paged_append.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p,
+        L.skvq_paged_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
                                         C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
-        L.skvq_paged_read.argtypes = [C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
-        L.skvq_paged_attention.argtypes = [C.c_void_p, C.POINTER(skvq_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+        L.skvq_paged_read.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.skvq_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                            C.c_void_p, C.c_void_p]
         L.skvq_paged_errors.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.c_void_p]
         L.skvq_paged_last_error.argtypes = [C.c_void_p]
@@ -459,11 +460,14 @@ class SkvqCache:
 # ---- rotary positions and the paged cache ------------------------------------------------------------------
 
 
+_ROPE_SIDE = struct.Struct("@PPqqqqqqi4x").pack   # skvq_rope_tensor
+
+
 def _stream_on(device: torch.device, stream) -> int:
     """The stream's handle; without one, the current stream of the tensors' device."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index or 0)
-    return int(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return stream.cuda_stream
 
 
 class SkvqRope:
@@ -506,35 +510,44 @@ class SkvqRope:
         """q, k [B][T][heads][head_dim] with any strides but the last dimension's; positions int32 [T] or [B][T], or
         None: start + t.  transpose: the gradient's way back.  Returns q's result, or (q's, k's); out_q / out_k may
         be q / k (in place)."""
-        xs, outs = ([q], [out_q]) if k is None else ([q, k], [out_q, out_k])
         if q.dtype not in DTYPES:
             raise ValueError(f"rotary positions take fp16, bf16 and fp32 tensors, got {q.dtype}")
+        if out_q is None:
+            out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        sides = self._side(q, out_q, q)
+        if k is not None:
+            if out_k is None:
+                out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            sides += self._side(k, out_k, q)
         b, t = q.shape[:2]
-        tensors = (skvq_rope_tensor * len(xs))()
-        for i, x in enumerate(xs):
-            if outs[i] is None:
-                outs[i] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            for y in (x, outs[i]):
-                if not (y.is_cuda and y.device == q.device and y.dtype == q.dtype and y.dim() == 4 and y.shape[:2] == (b, t)
-                        and y.shape == x.shape and y.shape[3] == self.head_dim and (y.stride(3) == 1 or y.numel() == 0)):
-                    raise ValueError(f"expected {q.dtype} tensors [{b}][{t}][heads][{self.head_dim}] on {q.device}, channels "
-                                     f"contiguous, got {y.dtype} {tuple(y.shape)} on {y.device}, strides {y.stride()}")
-            tensors[i] = skvq_rope_tensor(x.data_ptr(), outs[i].data_ptr(), *x.stride()[:3], *outs[i].stride()[:3], x.shape[2])
         at, stride = None, 0
         if positions is not None:
             if positions.dtype != torch.int32 or positions.device != q.device or positions.shape not in ((t,), (b, t)) or (
                     t > 1 and positions.stride(-1) != 1):
                 raise ValueError(f"positions must be int32 [{t}] or [{b}][{t}] on {q.device}")
             at, stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
-        call = (self._h, tensors, len(xs), DTYPES[q.dtype], b, t, at, stride, start, int(transpose), _stream_on(q.device, stream))
-        if q.device.index == torch._C._cuda_getDevice():
+        device = q.device.index
+        call = (self._h, sides, 1 if k is None else 2, DTYPES[q.dtype], b, t, at, stride, start, transpose,
+                torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+        if device == torch._C._cuda_getDevice():
             rc = lib().skvq_rope_apply(*call)
         else:
-            with torch.cuda.device(q.device):
+            with torch.cuda.device(device):
                 rc = lib().skvq_rope_apply(*call)
         if rc != SKVQ_OK:
             raise SkvqError(rc)
-        return outs[0] if k is None else (outs[0], outs[1])
+        return out_q if k is None else (out_q, out_k)
+
+    def _side(self, x, y, q) -> bytes:
+        """One skvq_rope_tensor (packed: a ctypes structure takes 2 us to fill)."""
+        shape, sx, sy = x.shape, x.stride(), y.stride()
+        if not (len(shape) == 4 and shape == y.shape and shape[:2] == q.shape[:2] and shape[3] == self.head_dim and x.is_cuda
+                and x.dtype == y.dtype == q.dtype and x.device == y.device == q.device
+                and (sx[3] == sy[3] == 1 or x.numel() == 0)):
+            raise ValueError(f"expected {q.dtype} tensors [{q.shape[0]}][{q.shape[1]}][heads][{self.head_dim}] on {q.device}, channels "
+                             f"contiguous, got {x.dtype} {tuple(x.shape)} on {x.device}, strides {sx}, and {y.dtype} "
+                             f"{tuple(y.shape)} on {y.device}, strides {sy}")
+        return _ROPE_SIDE(x.data_ptr(), y.data_ptr(), sx[0], sx[1], sx[2], sy[0], sy[1], sy[2], shape[2])
 
 
 class SkvqBatch:
@@ -562,6 +575,7 @@ class SkvqBatch:
 
         self.struct = skvq_batch(n, n_tokens, ptr(cu_tokens), ptr(seq_lens), ptr(page_table), page_table.shape[1], ptr(slots),
                                  ptr(positions), ptr(first))
+        self.address = C.addressof(self.struct)
 
 
 def make_paged_config(n_q_heads, n_kv_heads, group_size, window, page_size, n_pages, max_seqs, max_tokens, perm_k, perm_v,
@@ -639,17 +653,18 @@ class SkvqPagedCache:
 
     def _rows(self, t: torch.Tensor, n: int, heads: int) -> tuple[int, int]:
         """(address, elements between tokens) of rows [n][heads][D] whose heads lie one after the other."""
-        if not (t.dtype == self.dtype and t.device == self.device and t.shape == (n, heads, HEAD_DIM)
-                and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == HEAD_DIM)))):
+        stride = t.stride()
+        if t.dtype != self.dtype or t.device != self.device or t.shape != (n, heads, HEAD_DIM) or (
+                n and (stride[2] != 1 or (stride[1] != HEAD_DIM and heads > 1))):
             raise ValueError(f"expected {self.dtype} rows [{n}][{heads}][{HEAD_DIM}] on {self.device}, heads contiguous, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {stride}")
         # (the stride of a dimension of one token says nothing)
-        return t.data_ptr(), t.stride(0) if n > 1 else heads * HEAD_DIM
+        return t.data_ptr(), stride[0] if n > 1 else heads * HEAD_DIM
 
     def _batch(self, batch: SkvqBatch):
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
-        return C.byref(batch.struct), batch.n_tokens
+        return batch.address, batch.n_tokens
 
     def _new(self, n: int, heads: int, dtype=None):
         return torch.empty((n, heads, HEAD_DIM), dtype=dtype or self.dtype, device=self.device)

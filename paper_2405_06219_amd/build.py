@@ -29,7 +29,7 @@ UNITS = [
     ("skvq_decode_mfma.hip", "skvq_decode_mfma.o", []),
     ("skvq_paged_api.hip", "skvq_paged_api.o", []),
     ("skvq_rope.hip", "skvq_rope.o", []),
-    ("skvq_paged_rows.hip", "skvq_paged_rows.o", []),
+    ("skvq_paged_rows.hip", "skvq_paged_rows.o", ["-fno-honor-nans"]),
     ("skvq_paged_attn.hip", "skvq_paged_attn.o", []),
 ] + [("skvq_decode_mfma_inst.hip", f"skvq_decode_mfma_k{kl}_v{vl}.o", [f"-DSKVQ_KL={kl}", f"-DSKVQ_VL={vl}"])
      for kl, vl in DECODE_FORMATS]

@@ -10,32 +10,33 @@ namespace skvq {
 struct UnitDeal {
   int mul, div_log2, pad;
 };
-constexpr UnitDeal kAppendDeal{1, 2, 3};
-constexpr UnitDeal kReadDeal{1, 2, 2};
+constexpr UnitDeal kAppendDeal{1, 3, 3};
+constexpr UnitDeal kReadDeal{1, 3, 2};
 constexpr UnitDeal kTokenDeal{1, 0, 0};
 constexpr long long unit_start(const UnitDeal &d, int row0, int i) {
   return (((long long)row0 * d.mul) >> d.div_log2) + (long long)i * d.pad;
 }
 
-// Token a is packed row a - S.  Kernels take packed rows by fours (they share their value codes' bytes, and lie in one
-// page, whose size is a multiple of 16): tokens with the same (a + lead) / 4.
-constexpr int lead_of(int S) { return (4 - (S & 3)) & 3; }
+// Token a is packed row a - S.  Kernels take packed rows by eights (two fours, which share their value codes' bytes; an
+// eight lies in one page, whose size is a multiple of 16): tokens with the same (a + lead) / 8.
+constexpr int kEight = 8;
+constexpr int lead_of(int S) { return (kEight - S % kEight) % kEight; }
 
 // Append, with `len` tokens cached before and `total` after: the tokens that leave the window are [lo, hi) =
 // [max(0, len - W), total - W): ring rows and, of a long prompt, new tokens that never were in the ring.  A ring row is
 // overwritten by the lanes that have read it: those that pack old token a also write its successor, the newest token
-// of the same row.  Rows that held nothing (len < W) are fours of their own.
+// of the same row.  Rows that held nothing (len < W) are eights of their own.
 struct AppendPlan {
-  int W, S, total, len, lo, hi, lead, four0, leaving_fours, vacant_end, vacant_fours;
+  int W, S, total, len, lo, hi, lead, eight0, leaving, vacant_end, vacant;
 };
 constexpr AppendPlan append_plan(int total, int n_new, int W, int S) {
   AppendPlan p{W, S, total, total - n_new, 0, 0, lead_of(S), 0, 0, 0, 0};
   p.lo = p.len > W ? p.len - W : 0;
   p.hi = total - W > p.lo ? total - W : p.lo;
-  p.four0 = (p.lo + p.lead) >> 2;
-  p.leaving_fours = p.hi > p.lo ? ((p.hi + p.lead + 3) >> 2) - p.four0 : 0;
+  p.eight0 = (p.lo + p.lead) / kEight;
+  p.leaving = p.hi > p.lo ? (p.hi + p.lead + kEight - 1) / kEight - p.eight0 : 0;
   p.vacant_end = total < W ? total : W;
-  p.vacant_fours = p.len < p.vacant_end ? (p.vacant_end - p.len + 3) >> 2 : 0;
+  p.vacant = p.len < p.vacant_end ? (p.vacant_end - p.len + kEight - 1) / kEight : 0;
   return p;
 }
 struct AppendRow {
@@ -48,9 +49,9 @@ struct AppendRow {
   int ring;
 };
 constexpr AppendRow append_row(const AppendPlan &p, int unit, int r) {
-  AppendRow x{false, unit < p.leaving_fours, false, false, -1, -1, 0, -1};
+  AppendRow x{false, unit < p.leaving, false, false, -1, -1, 0, -1};
   if (x.leaving) {
-    const int a = 4 * (p.four0 + unit) + r - p.lead;
+    const int a = kEight * (p.eight0 + unit) + r - p.lead;
     x.valid = a >= p.lo && a < p.hi;
     x.token = a;
     x.old = a < p.len;
@@ -59,16 +60,18 @@ constexpr AppendRow append_row(const AppendPlan &p, int unit, int r) {
     x.fresh = x.old ? a + (p.total - 1 - a) / p.W * p.W : a;
     if (x.old) x.ring = a % p.W;
   } else {
-    x.ring = p.len + 4 * (unit - p.leaving_fours) + r;
+    x.ring = p.len + kEight * (unit - p.leaving) + r;
     x.valid = x.ring < p.vacant_end;
     x.fresh = x.ring + (p.total - 1 - x.ring) / p.W * p.W;
   }
   return x;
 }
 
-// Read of tokens [first, first + n): fours, and where a token is.
-constexpr int read_fours(int first, int n, int S) { return n > 0 ? ((first + n + lead_of(S) + 3) >> 2) - ((first + lead_of(S)) >> 2) : 0; }
-constexpr int read_token(int first, int S, int unit, int r) { return 4 * (((first + lead_of(S)) >> 2) + unit) + r - lead_of(S); }
+// Read of tokens [first, first + n): eights, and where a token is.
+constexpr int read_eights(int first, int n, int S) {
+  return n > 0 ? (first + n + lead_of(S) + kEight - 1) / kEight - (first + lead_of(S)) / kEight : 0;
+}
+constexpr int read_token(int first, int S, int unit, int r) { return kEight * ((first + lead_of(S)) / kEight + unit) + r - lead_of(S); }
 struct TokenPlace {
   bool full;  // in a row of k_rows / v_rows, else packed row `row`
   int row;

@@ -1,13 +1,14 @@
 // skvq_paged_append and skvq_paged_read: tokens into the paged cache and back out (Section 3.2, Eq. 2).
 //
-// Both work on fours of packed rows (four rows share their value codes' 256 bytes): one workgroup takes a
-// four of one sequence and some kv heads, one wavefront one head's keys or values at a time.  Lane (r, m) =
-// (lane / 16, lane % 16) holds row r's channels 8m .. 8m+7 as they come and go, 16 bytes; as codes it holds
-// dword m of a key row, or row r's part of value piece m, eight reordered positions either way.  The reorder
-// goes through LDS, a row of halves per (wavefront, r).
+// Both work on eights of packed rows: one workgroup takes an eight of one sequence and some kv heads, one wavefront one
+// head's keys or values at a time.  Lane (r, m) = (lane / 8, lane % 8) holds sixteen of row r's channels as they come and
+// go, two pieces of 16 bytes that hold both members of the pairs it rotates (LanePieces); as codes it holds two dwords of
+// a key row, of the same quantization groups, or row r's part of two value pieces: sixteen reordered positions either
+// way.  The reorder goes through LDS, a row of values per (wavefront, r).
 //
-// Bound by memory for prompts (a row's 512 bytes in, 140 out), by the chain of dependent loads for decode
-// steps: sequence, its counts, its page, its ring row.
+// Bound by memory and vector instructions for prompts (a row's 512 bytes in, 140 out; eight channels a lane and four rows
+// a wavefront took twice as long: what a group needs once is computed by all its lanes), by the chain of dependent loads
+// for decode steps: sequence, its counts, its page, its ring row.
 #include <hip/hip_runtime.h>
 
 #include "skvq_append_device.h"
@@ -17,7 +18,6 @@ namespace skvq {
 namespace {
 
 constexpr int kRowStride = 136;  // values per parked row: 272 B, so the rows' channels fall in different banks
-constexpr int kRor4 = 0x124, kRor8 = 0x128;
 
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -77,128 +77,179 @@ __device__ __forceinline__ void rotate_queries(const PagedLayout &L, const RopeT
     return true;
   };
   const bool copy = q.q != q.out;
-  if (tab.half % 8 == 0)
-    rope_walk<T, 8>(tab, cs, q.tokens_per_group, kD, copy, L.Hq, rows);
+  if (rope_streams(tab.half, kD, sizeof(T)))
+    rope_walk<T, 8, true>(tab, cs, q.tokens_per_group, kD, copy, L.Hq, rows);
+  else if (tab.half % 8 == 0)
+    rope_walk<T, 8, false>(tab, cs, q.tokens_per_group, kD, copy, L.Hq, rows);
   else
-    rope_walk<T, 1>(tab, cs, q.tokens_per_group, kD, copy, L.Hq, rows);
+    rope_walk<T, 1, false>(tab, cs, q.tokens_per_group, kD, copy, L.Hq, rows);
 }
 
-// What a lane's eight rotated channels need: its own cosines and sines (1 and 0 behind the rotated part).
-struct LaneRotation {
-  float c[8], s[8];
+// The channels of a lane's two pieces: of half layout in whole pieces both members of pairs 8m .., else neighbours.
+struct LanePieces {
+  int a, b;    // first channels
+  bool turns;  // both members of every pair are the lane's own, and there are some
 };
-__device__ __forceinline__ LaneRotation lane_rotation(const RopeTable &tab, const float2 *cs, int m) {
-  LaneRotation t;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int ch = 8 * m + e;
-    t.c[e] = 1.0f;
-    t.s[e] = 0.0f;
-    if (ch < 2 * tab.half) {
-      const bool first = tab.interleaved ? !(ch & 1) : ch < tab.half;
-      const float2 f = cs[tab.interleaved ? ch >> 1 : first ? ch : ch - tab.half];
-      t.c[e] = f.x;
-      t.s[e] = first ? -f.y : f.y;
-    }
-  }
-  return t;
+__device__ __forceinline__ LanePieces lane_pieces(const RopeTable &tab, int m) {
+  const int half = tab.half;
+  if (half % 8 || tab.interleaved) return LanePieces{16 * m, 16 * m + 8, half % 8 == 0 && 16 * m < 2 * half};
+  if (8 * m < half) return LanePieces{8 * m, half + 8 * m, true};
+  return LanePieces{16 * m, 16 * m + 8, false};  // (lanes half/8 .. 7 have the channels from 2 half on)
 }
-// row: this row's place in LDS (kRowStride values), used on the way
+
+// Sixteen channels of a row on their way to codes.
 template <class T>
-__device__ __forceinline__ Piece<T, 8> rotated(const RopeTable &tab, const LaneRotation &t, const Piece<T, 8> &x, T *row, int m) {
-  Piece<T, 8> other, y;
-  if (tab.interleaved) {
+struct Pieces {
+  Piece<T, 8> a, b;
+};
+template <class T>
+__device__ __forceinline__ Pieces<T> load_pieces(const T *row, const LanePieces &at) {
+  return Pieces<T>{*reinterpret_cast<const Piece<T, 8> *>(row + at.a), *reinterpret_cast<const Piece<T, 8> *>(row + at.b)};
+}
+template <class T>
+__device__ __forceinline__ void store_pieces(T *row, const LanePieces &at, const Pieces<T> &x) {
+  *reinterpret_cast<Piece<T, 8> *>(row + at.a) = x.a;
+  *reinterpret_cast<Piece<T, 8> *>(row + at.b) = x.b;
+}
+// Rotates them.  c, s: cosines and sines of the lane's eight pairs (turns).  Rotated parts that do not fill pieces go
+// channel by channel through LDS (row: this row's place; cs: the row's cosines and sines).
+template <class T>
+__device__ __forceinline__ void rotate_pieces(const RopeTable &tab, const LanePieces &at, const float (&c)[8], const float (&s)[8],
+                                              const float2 *cs, T *row, Pieces<T> &x) {
+  const int half = tab.half;
+  if (half % 8 == 0) {
+    if (!at.turns) return;
+    Pieces<T> y;
+    if (tab.interleaved) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) other[e] = x[e ^ 1];
-  } else {
-    *reinterpret_cast<Piece<T, 8> *>(row + 8 * m) = x;
-    wave_lds_sync();
-    const int ch = 8 * m, half = tab.half;
-    if (half % 8 == 0) {
-      const int at = ch < half ? ch + half : ch < 2 * half ? ch - half : ch;
-      other = *reinterpret_cast<const Piece<T, 8> *>(row + at);
+      for (int e = 0; e < 8; e += 2) {
+        const int f = e / 2, g = 4 + e / 2;
+        y.a[e] = (T)rope_turned((float)x.a[e], (float)x.a[e + 1], c[f], -s[f]);
+        y.a[e + 1] = (T)rope_turned((float)x.a[e + 1], (float)x.a[e], c[f], s[f]);
+        y.b[e] = (T)rope_turned((float)x.b[e], (float)x.b[e + 1], c[g], -s[g]);
+        y.b[e + 1] = (T)rope_turned((float)x.b[e + 1], (float)x.b[e], c[g], s[g]);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = ch + e;
-        other[e] = row[c < half ? c + half : c < 2 * half ? c - half : c];
+        y.a[e] = (T)rope_turned((float)x.a[e], (float)x.b[e], c[e], -s[e]);
+        y.b[e] = (T)rope_turned((float)x.b[e], (float)x.a[e], c[e], s[e]);
       }
     }
-    wave_lds_sync();
+    x = y;
+    return;
   }
+  store_pieces(row, at, x);
+  wave_lds_sync();
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int ch = 8 * m + e;
-    const T z = (T)rope_turned((float)x[e], (float)other[e], t.c[e], t.s[e]);
-    y[e] = ch < 2 * tab.half ? z : x[e];
+  for (int e = 0; e < 16; ++e) {
+    const int ch = (e < 8 ? at.a : at.b - 8) + e;
+    if (ch < 2 * half) {
+      const bool first = tab.interleaved ? !(ch & 1) : ch < half;
+      const float2 f = cs[tab.interleaved ? ch >> 1 : first ? ch : ch - half];
+      const float other = (float)row[tab.interleaved ? ch ^ 1 : first ? ch + half : ch - half];
+      const float own = (float)(e < 8 ? x.a[e & 7] : x.b[e & 7]);
+      const T y = (T)rope_turned(own, other, f.x, first ? -f.y : f.y);
+      if (e < 8)
+        x.a[e & 7] = y;
+      else
+        x.b[e & 7] = y;
+    }
   }
-  return y;
+  wave_lds_sync();
 }
 
 __device__ __forceinline__ unsigned long long lane_bytes(const uint8_t *p) { return *reinterpret_cast<const unsigned long long *>(p); }
 __device__ __forceinline__ int byte_of(unsigned long long w, int e) { return (int)((w >> (8 * e)) & 0xffu); }
-constexpr int key_nibble(int e) { return e % 2 ? 4 + e / 2 : e / 2; }
+// The element of a dword of key codes in nibble n: (0, 2, 4, 6, 1, 3, 5, 7).
+constexpr int key_element(int n) { return n < 4 ? 2 * n : 2 * n - 7; }
+// A lane's two dwords of a key row, and its two value pieces.
+__device__ __forceinline__ int key_dword(int m, int i) { return 4 * (2 * (m & 1) + i) + (m >> 1); }  // 4g + j: g = 2 (m % 2) + i, j = m / 2
+__device__ __forceinline__ int value_piece(int m, int i) { return 2 * m + i; }
 
-// Quantizes a four's key rows of one head (parked in LDS) and stores codes and pairs.  part: the head's part
-// of the page, or null; rp: the row's place in it.
+// code = rint(clamp(y, 0, 15)), y = (x - lo) * inv with each operation rounded once: clamping first gives the same integer,
+// and adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves the code in the low bits.
+__device__ __forceinline__ unsigned code_in_low_bits(float x, const GroupParams &gp) {
+#pragma clang fp contract(off)
+  const float d = x - gp.lo;
+  const float y = d * gp.inv;
+  return __float_as_uint(__builtin_amdgcn_fmed3f(y, 0.0f, 15.0f) + 12582912.0f);
+}
+
+// Quantizes an eight's key rows of one head (parked in LDS) and stores codes and pairs.  part: the head's part
+// of the page, or null; rp: the row's place in it.  channels: those of the lane's two dwords.
 template <class T, int NG>
-__device__ __forceinline__ void pack_keys(const PagedLayout &L, const T *row, unsigned long long channels, const float *clip,
+__device__ __forceinline__ void pack_keys(const PagedLayout &L, const T *row, const unsigned long long (&channels)[2], const float *clip,
                                           uint8_t *part, int rp, int m) {
-  float x[8], mn, mx;
+  float x[2][8], mn, mx;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    x[e] = (float)row[byte_of(channels, e)];
-    mn = e ? fminf(mn, x[e]) : x[e];
-    mx = e ? fmaxf(mx, x[e]) : x[e];
-  }
-  // dword m = 4g + j holds positions 32j + 8g ..: a group is the lanes of one j (NG = 4), of a pair, or all
-  minmax_with<kRor8>(mn, mx);
-  minmax_with<kRor4>(mn, mx);
-  if (NG <= 2) minmax_with<kLaneXor1>(mn, mx);
-  if (NG == 1) minmax_with<kLaneXor2>(mn, mx);
-  const int g = (m & 3) * NG / 4;
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[i][e] = (float)row[byte_of(channels[i], e)];
+      mn = i + e ? fminf(mn, x[i][e]) : x[i][e];
+      mx = i + e ? fmaxf(mx, x[i][e]) : x[i][e];
+    }
+  // dword 4g + j holds positions 32j + 8g ..: a group is the two lanes of one j (NG = 4), four lanes, or all eight
+  minmax_with<kLaneXor1>(mn, mx);
+  if (NG <= 2) minmax_with<kLaneXor2>(mn, mx);
+  if (NG == 1) minmax_with<kMirror8>(mn, mx);
+  const int g = (m >> 1) * NG / 4;
   const GroupParams gp = group_params(mn, mx, clip[g], 15.0f, L.meta_fmt);
-  unsigned w = 0;
+  unsigned w[2] = {0u, 0u};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w |= encode(x[e], gp, 15.0f) << (4 * key_nibble(e));
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int n = 0; n < 8; ++n) w[i] = __builtin_amdgcn_alignbit(code_in_low_bits(x[i][key_element(n)], gp), w[i], 4);
   if (part) {
-    reinterpret_cast<unsigned *>(part + rp * (kD / 2))[m] = w;
-    if (m < 4 && m % (4 / NG) == 0)
-      meta_store_pair(part + L.km_at, rp * NG + g, MetaPair{gp.scale, gp.lo, gp.stored}, L.meta_fmt);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) reinterpret_cast<unsigned *>(part + rp * (kD / 2))[key_dword(m, i)] = w[i];
+    if (m % (8 / NG) == 0) meta_store_pair(part + L.km_at, rp * NG + g, MetaPair{gp.scale, gp.lo, gp.stored}, L.meta_fmt);
   }
 }
 
-// ... its value rows: lane (r, m) holds positions 16n + m, n = 0 .. 7, some of every group.
+// ... its value rows: the lane's pieces hold positions 16n + piece, n = 0 .. 7, some of every group.
 template <class T, int NG>
-__device__ __forceinline__ void pack_values(const PagedLayout &L, const T *row, unsigned long long channels, const float *clip,
+__device__ __forceinline__ void pack_values(const PagedLayout &L, const T *row, const unsigned long long (&channels)[2], const float *clip,
                                             uint8_t *part, int rp, int m) {
   unsigned w[2] = {0u, 0u};
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    float x[8 / NG], mn, mx;
+    float x[2][8 / NG], mn, mx;
 #pragma unroll
-    for (int e = 0; e < 8 / NG; ++e) {
-      x[e] = (float)row[byte_of(channels, g * (8 / NG) + e)];
-      mn = e ? fminf(mn, x[e]) : x[e];
-      mx = e ? fmaxf(mx, x[e]) : x[e];
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 8 / NG; ++e) {
+        x[i][e] = (float)row[byte_of(channels[i], g * (8 / NG) + e)];
+        mn = i + e ? fminf(mn, x[i][e]) : x[i][e];
+        mx = i + e ? fmaxf(mx, x[i][e]) : x[i][e];
+      }
     minmax_with<kLaneXor1>(mn, mx);
     minmax_with<kLaneXor2>(mn, mx);
     minmax_with<kMirror8>(mn, mx);
-    minmax_with<kMirror16>(mn, mx);
     const GroupParams gp = group_params(mn, mx, clip[g], 15.0f, L.meta_fmt);
 #pragma unroll
-    for (int e = 0; e < 8 / NG; ++e) {
-      const int n = g * (8 / NG) + e;
-      w[n / 4] |= encode(x[e], gp, 15.0f) << (4 * (n % 4));
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 8 / NG; ++e) w[i] = __builtin_amdgcn_alignbit(code_in_low_bits(x[i][e], gp), w[i], 4);
     if (part && m == g) meta_store_pair(part + L.vm_at, rp * NG + g, MetaPair{gp.scale, gp.lo, gp.stored}, L.meta_fmt);
   }
-  if (part) {
-    const int r = rp & 3;
-    unsigned short *to = reinterpret_cast<unsigned short *>(part + L.v_at + (rp >> 2) * (2 * kD) + 16 * m + 8 * (r >> 1) + 2 * (r & 1));
-    to[0] = (unsigned short)w[0];
-    to[2] = (unsigned short)w[1];
+  // Two rows of a four share dwords: row 2p the low halves of both.  Where both are stored each lane takes one dword per
+  // piece (the even row's the first four positions), else each its own halves.  (Lane ^ 8 is the row beside it.)
+  const bool odd = rp & 1;
+  const int here = part ? 1 : 0;
+  const bool both = here & __builtin_amdgcn_update_dpp(0, here, 0x128, 0xF, 0xF, true);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(odd ? w[i] & 0xffffu : w[i] >> 16), 0x128, 0xF, 0xF, true);
+    uint8_t *at = part + L.v_at + (rp >> 2) * (2 * kD) + 16 * value_piece(m, i) + 8 * ((rp & 3) >> 1);
+    if (both) {
+      reinterpret_cast<unsigned *>(at)[odd] = odd ? got | (w[i] & 0xffff0000u) : (w[i] & 0xffffu) | (got << 16);
+    } else if (part) {
+      unsigned short *to = reinterpret_cast<unsigned short *>(at) + odd;
+      to[0] = (unsigned short)w[i];
+      to[2] = (unsigned short)(w[i] >> 16);
+    }
   }
 }
 
@@ -207,60 +258,69 @@ template <class T, int NG>
 __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedLayout L, const RopeTable tab, const PagedBatch b,
                                                                     const TokenRows k, const TokenRows v, const QueryRows q,
                                                                     unsigned n_units, int heads_per_group) {
-  __shared__ float2 cs[kRopeMaxTokens][kRopeMaxPairs];
-  __shared__ __align__(16) T parked[4][4][kRowStride];
+  __shared__ float2 cs[kEight][kRopeMaxPairs / 2];  // (a head of 128 channels has 64 pairs)
+  __shared__ __align__(16) T parked[4][kEight][kRowStride];
   if (blockIdx.x >= n_units) {
-    if (blockIdx.y == 0) rotate_queries<T>(L, tab, b, q, blockIdx.x - n_units, cs);
+    static_assert(sizeof cs >= sizeof(float2[kRopeMaxTokens][kRopeMaxPairs]), "queries use it with a stride of their own");
+    if (blockIdx.y == 0) rotate_queries<T>(L, tab, b, q, blockIdx.x - n_units, reinterpret_cast<float2(*)[kRopeMaxPairs]>(cs));
     return;
   }
-  typedef Piece<T, 8> P;
   const int i = sequence_of_unit(b, blockIdx.x, kAppendDeal);
   const Sequence s = sequence_of(b, L, i);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 4, m = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 3, m = lane & 7;
   const long long unit = blockIdx.x - unit_start(kAppendDeal, s.row0, i);
   if (!s.counts_ok || !s.slot_ok) {
     if (threadIdx.x == 0) atomicOr(L.errors, s.counts_ok ? SKVQ_PAGED_BAD_SLOT : SKVQ_PAGED_BAD_COUNTS);
     return;
   }
   const AppendPlan plan = append_plan(s.total, s.n_new, L.W, L.S);
-  if (unit < 0 || unit >= plan.leaving_fours + plan.vacant_fours) return;
+  if (unit < 0 || unit >= plan.leaving + plan.vacant) return;
   const AppendRow x = append_row(plan, (int)unit, r);  // this lane's row
   const long long token = s.row0 + (x.fresh - plan.len);  // (of valid rows: a row of k and v)
-  if (x.valid && tab.half) {
-    // (sixteen lanes of each wavefront per row, all wavefronts together: 64 threads)
-    const int position = b.positions ? b.positions[token] : x.fresh;
-    for (int p = 16 * wave + m; p < tab.half; p += 64) cs[r][p] = rope_cos_sin(tab.turn[p], position, tab.amplitude);
-  }
   uint8_t *page = nullptr;
   if (x.valid && x.leaving && !x.sink) page = page_of(L, b, i, x.te);
+  if (x.valid && tab.half) {
+    // (eight lanes of each wavefront per row, all wavefronts together: 32 threads)
+    const int position = b.positions ? b.positions[token] : x.fresh;
+    for (int p = 8 * wave + m; p < tab.half; p += 32) cs[r][p] = rope_cos_sin(tab.turn[p], position, tab.amplitude);
+  }
   __syncthreads();
   const bool keys = wave < 2;  // wavefronts 0, 1: keys; 2, 3: values
-  LaneRotation turn;
-  if (keys) turn = lane_rotation(tab, cs[r], m);
+  const LanePieces at = lane_pieces(tab, m);
+  float c[8], sn[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float2 f = keys && at.turns ? cs[r][8 * m + e] : make_float2(1.0f, 0.0f);
+    c[e] = f.x;
+    sn[e] = f.y;
+  }
   const TokenRows src = keys ? k : v;
   T *rows = reinterpret_cast<T *>(keys ? L.k_rows : L.v_rows) + (long long)s.slot * L.Hk * (L.W + L.S) * kD;
   T *row = parked[wave][r];
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
-    T *head_rows = rows + (long long)h * (L.W + L.S) * kD + 8 * m;
-    P fresh = {}, gone = {};
+    T *head_rows = rows + (long long)h * (L.W + L.S) * kD;
+    const uint8_t *order = (keys ? L.k_channel : L.v_channel) + h * kD;
+    const unsigned long long channels[2] = {lane_bytes(order + 8 * (keys ? key_dword(m, 0) : value_piece(m, 0))),
+                                            lane_bytes(order + 8 * (keys ? key_dword(m, 1) : value_piece(m, 1)))};
+    Pieces<T> fresh = {}, gone = {};
     if (x.valid) {
-      fresh = *reinterpret_cast<const P *>((const T *)src.p + token * src.stride + h * kD + 8 * m);
-      if (x.old) gone = *reinterpret_cast<const P *>(head_rows + (long long)x.ring * kD);
+      fresh = load_pieces((const T *)src.p + token * src.stride + h * kD, at);
+      if (x.old) gone = load_pieces(head_rows + (long long)x.ring * kD, at);
     }
-    if (keys && tab.half) fresh = rotated(tab, turn, fresh, row, m);
-    if (x.valid && x.ring >= 0) *reinterpret_cast<P *>(head_rows + (long long)x.ring * kD) = fresh;
+    if (keys && tab.half) rotate_pieces(tab, at, c, sn, cs[r], row, fresh);
+    if (x.valid && x.ring >= 0) store_pieces(head_rows + (long long)x.ring * kD, at, fresh);
     if (!x.leaving) continue;
     if (!x.old) gone = fresh;
-    if (x.valid && x.sink) *reinterpret_cast<P *>(head_rows + (long long)(L.W + x.token) * kD) = gone;
-    *reinterpret_cast<P *>(row + 8 * m) = gone;
+    if (x.valid && x.sink) store_pieces(head_rows + (long long)(L.W + x.token) * kD, at, gone);
+    store_pieces(row, at, gone);
     wave_lds_sync();
     uint8_t *part = page ? page + (long long)h * L.part_bytes : nullptr;
     const int rp = x.te & ((1 << L.page_log2) - 1);
     if (keys)
-      pack_keys<T, NG>(L, row, lane_bytes(L.k_channel + h * kD + 8 * m), L.clip_k + h * NG, part, rp, m);
+      pack_keys<T, NG>(L, row, channels, L.clip_k + h * NG, part, rp, m);
     else
-      pack_values<T, NG>(L, row, lane_bytes(L.v_channel + h * kD + 8 * m), L.clip_v + h * NG, part, rp, m);
+      pack_values<T, NG>(L, row, channels, L.clip_v + h * NG, part, rp, m);
     wave_lds_sync();
   }
 }
@@ -275,11 +335,10 @@ __device__ __forceinline__ float dequantized(unsigned code, float2 pair) {
 template <class T, int NG>
 __global__ __launch_bounds__(kRopeThreads) void paged_read_kernel(const PagedLayout L, const PagedBatch b, T *k, long long k_stride,
                                                                   T *v, long long v_stride, int heads_per_group) {
-  __shared__ __align__(16) T parked[4][4][kRowStride];
-  typedef Piece<T, 8> P;
+  __shared__ __align__(16) T parked[4][kEight][kRowStride];
   const int i = sequence_of_unit(b, blockIdx.x, kReadDeal);
   const Sequence s = sequence_of(b, L, i);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 4, m = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 3, m = lane & 7;
   const long long unit = blockIdx.x - unit_start(kReadDeal, s.row0, i);
   const int f = b.first ? b.first[i] : s.total - s.n_new;
   const bool range_ok = f >= 0 && f <= s.total - s.n_new;
@@ -288,53 +347,58 @@ __global__ __launch_bounds__(kRopeThreads) void paged_read_kernel(const PagedLay
       atomicOr(L.errors, !s.counts_ok ? SKVQ_PAGED_BAD_COUNTS : !s.slot_ok ? SKVQ_PAGED_BAD_SLOT : SKVQ_PAGED_BAD_RANGE);
     return;
   }
-  if (unit < 0 || unit >= read_fours(f, s.n_new, L.S)) return;
+  if (unit < 0 || unit >= read_eights(f, s.n_new, L.S)) return;
   const int a = read_token(f, L.S, (int)unit, r);
   bool valid = a >= f && a < f + s.n_new;
-  const TokenPlace at = token_place(a, s.total, L.W, L.S);
-  const bool full = at.full;
+  const TokenPlace place = token_place(a, s.total, L.W, L.S);
+  const bool full = place.full;
   const uint8_t *page = nullptr;
   if (valid && !full) {
-    page = page_of(L, b, i, at.row);
+    page = page_of(L, b, i, place.row);
     valid = page != nullptr;
   }
-  const int rp = at.row & ((1 << L.page_log2) - 1);
+  const int rp = place.row & ((1 << L.page_log2) - 1);
   const bool keys = wave < 2;
   T *to = keys ? k : v;
   if (!to) return;
-  to += (s.row0 + (long long)(a - f)) * (keys ? k_stride : v_stride) + 8 * m;
+  to += (s.row0 + (long long)(a - f)) * (keys ? k_stride : v_stride);
   const T *rows = reinterpret_cast<const T *>(keys ? L.k_rows : L.v_rows) + (long long)s.slot * L.Hk * (L.W + L.S) * kD;
   T *row = parked[wave][r];
+  const LanePieces at = {8 * m, kD / 2 + 8 * m, false};  // (whole lines per instruction)
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
-    P x = {};
-    if (valid && full) x = *reinterpret_cast<const P *>(rows + ((long long)h * (L.W + L.S) + at.row) * kD + 8 * m);
+    Pieces<T> x = {};
+    if (valid && full) x = load_pieces(rows + ((long long)h * (L.W + L.S) + place.row) * kD, at);
     if (valid && !full) {
-      const uint8_t *part = page + (long long)h * L.part_bytes;
-      if (keys) {
-        const unsigned w = reinterpret_cast<const unsigned *>(part + rp * (kD / 2))[m];
-        const float2 pair = meta_load_pair(part + L.km_at, rp * NG + (m & 3) * NG / 4, L.meta_fmt);
-        const unsigned long long ch = lane_bytes(L.k_channel + h * kD + 8 * m);
+      const uint8_t *part = page + (long long)h * L.part_bytes, *order = (keys ? L.k_channel : L.v_channel) + h * kD;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) row[byte_of(ch, e)] = (T)dequantized((w >> (4 * key_nibble(e))) & 15u, pair);
-      } else {
-        const unsigned short *halves = reinterpret_cast<const unsigned short *>(part + L.v_at + (rp >> 2) * (2 * kD) + 16 * m + 8 * ((rp & 3) >> 1) + 2 * (rp & 1));
-        const unsigned w = halves[0] | ((unsigned)halves[2] << 16);
-        const unsigned long long ch = lane_bytes(L.v_channel + h * kD + 8 * m);
+      for (int i = 0; i < 2; ++i) {
+        if (keys) {
+          const unsigned w = reinterpret_cast<const unsigned *>(part + rp * (kD / 2))[key_dword(m, i)];
+          const unsigned long long ch = lane_bytes(order + 8 * key_dword(m, i));
+          const float2 pair = meta_load_pair(part + L.km_at, rp * NG + (m >> 1) * NG / 4, L.meta_fmt);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const float2 pair = meta_load_pair(part + L.vm_at, rp * NG + g, L.meta_fmt);
+          for (int n = 0; n < 8; ++n) row[byte_of(ch, key_element(n))] = (T)dequantized((w >> (4 * n)) & 15u, pair);
+        } else {
+          // the row's halves of two dwords
+          const uint2 two = *reinterpret_cast<const uint2 *>(part + L.v_at + (rp >> 2) * (2 * kD) + 16 * value_piece(m, i) + 8 * ((rp & 3) >> 1));
+          const unsigned w = __builtin_amdgcn_perm(two.y, two.x, rp & 1 ? 0x07060302u : 0x05040100u);
+          const unsigned long long ch = lane_bytes(order + 8 * value_piece(m, i));
 #pragma unroll
-          for (int e = 0; e < 8 / NG; ++e) {
-            const int n = g * (8 / NG) + e;
-            row[byte_of(ch, n)] = (T)dequantized((w >> (4 * n)) & 15u, pair);
+          for (int g = 0; g < NG; ++g) {
+            const float2 pair = meta_load_pair(part + L.vm_at, rp * NG + g, L.meta_fmt);
+#pragma unroll
+            for (int e = 0; e < 8 / NG; ++e) {
+              const int n = g * (8 / NG) + e;
+              row[byte_of(ch, n)] = (T)dequantized((w >> (4 * n)) & 15u, pair);
+            }
           }
         }
       }
     }
     wave_lds_sync();
-    if (!full) x = *reinterpret_cast<const P *>(row + 8 * m);
-    if (valid) *reinterpret_cast<P *>(to + h * kD) = x;
+    if (!full) x = load_pieces((const T *)row, at);
+    if (valid) store_pieces(to + h * kD, at, x);
     wave_lds_sync();
   }
 }
@@ -377,8 +441,8 @@ hipError_t launch_paged_append(const PagedLayout &L, const RopeTable &tab, const
                                TokenRows q, void *q_out, long long q_out_stride, int n_cus, hipStream_t s) {
   const PagedBatch b = batch_of(batch);
   const long long units = units_of(batch, kAppendDeal);
-  // (as in skvq_rope_apply: four tokens a workgroup once that leaves enough of them)
-  const QueryRows query{q.p, q_out, q.stride, q_out_stride, b.n_tokens >= 4096 ? kRopeMaxTokens : 1};
+  const int pieces = (q.p != q_out ? kD : 2 * tab.half) / (tab.half % 8 ? 1 : 8) / 2;
+  const QueryRows query{q.p, q_out, q.stride, q_out_stride, rope_tokens_per_group(b.n_tokens, pieces > 0 ? pieces : 1, L.Hq)};
   const unsigned groups = q.p && (tab.half || q.p != q_out) ? (b.n_tokens + query.tokens_per_group - 1) / query.tokens_per_group : 0;
   const int heads = heads_per_group(L.Hk, units, n_cus);
   return L.dtype == SKVQ_DTYPE_BF16 ? launch_append<__bf16>(L, tab, b, k, v, query, (unsigned)units, groups, heads, s)

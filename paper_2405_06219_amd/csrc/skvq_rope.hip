@@ -27,7 +27,7 @@ struct RopeArgs {
 };
 
 // V: channels per access, 16 bytes' worth or 1.
-template <class T, int V>
+template <class T, int V, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeTable tab, const RopeArgs a) {
   __shared__ float2 cs[kRopeMaxTokens][kRopeMaxPairs];
   const int half = tab.half, n_here = a.tokens_per_group;
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeTable tab,
     }
   }
   __syncthreads();
-  rope_walk<T, V>(tab, cs, n_here, a.head_dim, a.copy_rest, a.n_heads, [&](int k, int h, const T *&from, T *&to) {
+  rope_walk<T, V, STREAM>(tab, cs, n_here, a.head_dim, a.copy_rest, a.n_heads, [&](int k, int h, const T *&from, T *&to) {
     const unsigned token = first + k;
     if (token >= a.total) return false;
     const unsigned b = token / a.n_tokens, t = token - b * a.n_tokens;
@@ -60,10 +60,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeTable tab,
 template <class T>
 hipError_t launch_typed(const RopeTable &tab, const RopeArgs &a, bool wide, unsigned groups, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  if (wide)
-    rope_kernel<T, V><<<groups, kRopeThreads, 0, s>>>(tab, a);
+  if (wide && rope_streams(tab.half, a.head_dim, sizeof(T)))
+    rope_kernel<T, V, true><<<groups, kRopeThreads, 0, s>>>(tab, a);
+  else if (wide)
+    rope_kernel<T, V, false><<<groups, kRopeThreads, 0, s>>>(tab, a);
   else
-    rope_kernel<T, 1><<<groups, kRopeThreads, 0, s>>>(tab, a);
+    rope_kernel<T, 1, false><<<groups, kRopeThreads, 0, s>>>(tab, a);
   return hipGetLastError();
 }
 
@@ -80,19 +82,17 @@ hipError_t launch_rope(const RopeTable &tab, int head_dim, const skvq_rope_tenso
   for (int i = 0; i < n_tensors; ++i) {
     const skvq_rope_tensor &t = tensors[i];
     a.side[i] = RopeSide{t.x, t.y, t.x_batch, t.x_token, t.x_head, t.y_batch, t.y_token, t.y_head};
+    a.n_heads += t.n_heads;
     wide = wide && !(((uintptr_t)t.x | (uintptr_t)t.y) & 15);
     for (long long d : {t.x_batch, t.x_token, t.x_head, t.y_batch, t.y_token, t.y_head}) wide = wide && d % V == 0;
     copy = copy || t.x != t.y;
-    a.n_heads += t.n_heads;
   }
   a.first_heads = tensors[0].n_heads;
   a.head_dim = head_dim;
   a.copy_rest = copy && 2 * tab.half < head_dim;
   a.n_tokens = n_tokens;
   a.total = n_tokens * (unsigned)batch;
-  // four tokens a workgroup, where that leaves enough workgroups for the 256 compute units: one token a
-  // workgroup leaves three quarters of the threads without a cosine to compute
-  a.tokens_per_group = a.total >= 4096u ? kRopeMaxTokens : 1;
+  a.tokens_per_group = rope_tokens_per_group(a.total, (a.copy_rest ? head_dim : 2 * tab.half) / (wide ? V : 1) / 2, a.n_heads);
   a.positions = positions;
   a.positions_batch = positions_batch;
   a.start = start;

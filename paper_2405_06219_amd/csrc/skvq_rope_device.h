@@ -58,13 +58,15 @@ __device__ __forceinline__ float rope_turned(float x, float other, float c, floa
 }
 
 // The rotation of a group of tokens by a workgroup of kRopeThreads.  cs: their cosines and sines, [token][pair],
-// in LDS.  rows(k, h, &from, &to): head h's rows of token k of the group, false where there is no such token.
+// in LDS.  rows(k, h, &from, &to): head h's rows of token k, false where there is no such token.
 //
 // A thread keeps the cosines and sines of its place in the head in registers and walks over the heads, two
-// pieces of V channels (both members of V pairs) per step, kRopeAhead steps' loads in flight.
+// pieces of V channels (2V members of V pairs) per head.  Few registers for many wavefronts, and STREAMing accesses
+// where an instruction takes whole cache lines: a 32k prompt's rotation (671 MB) takes 121 - 123 us, with plain accesses
+// and four heads' loads in flight 140.
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxTokens = 4;  // tokens per workgroup
-constexpr int kRopeAhead = 4;
+constexpr int kRopeAhead = 2;
 constexpr int kRopeMaxPairs = SKVQ_ROPE_MAX_HEAD_DIM / 2;
 
 // V values as one access.  (A vector type: a struct around an array may be moved to LDS by the compiler, whose addressing
@@ -72,27 +74,46 @@ constexpr int kRopeMaxPairs = SKVQ_ROPE_MAX_HEAD_DIM / 2;
 template <class T, int V>
 using Piece = T __attribute__((ext_vector_type(V)));
 
-template <class T, int V, class Rows>
-__device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*cs)[kRopeMaxPairs], int n_here,
-                                          int head_dim, bool copy_rest, int n_heads, Rows rows) {
+template <bool STREAM, class P>
+__device__ __forceinline__ P piece_load(const P *p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p); else return *p;
+}
+template <bool STREAM, class P>
+__device__ __forceinline__ void piece_store(P *p, P x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, p); else *p = x;
+}
+// Tokens per workgroup: about five heads a thread (more wait for memory in turn, fewer compute cosines for too little),
+// one token where workgroups are few.
+inline int rope_tokens_per_group(long long tokens, long long pieces, long long heads) {
+  if (tokens < 4096) return 1;
+  const long long n = 5 * kRopeThreads / (pieces * heads);
+  return n >= kRopeMaxTokens ? kRopeMaxTokens : n >= 2 ? 2 : 1;
+}
+// whether each of the two pieces' runs over a head fills whole lines (of rows that begin on one)
+inline __host__ __device__ bool rope_streams(int half, int head_dim, int size) { return half * size % 128 == 0 && head_dim * size % 128 == 0; }
+
+template <class T, int V, bool STREAM, class Rows>
+__device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*cs)[kRopeMaxPairs], int n_here, int head_dim,
+                                          bool copy_rest, int n_heads, Rows rows) {
   typedef Piece<T, V> P;
-  const int half = tab.half, rotated = half / V, pieces = rotated + (copy_rest ? (head_dim - 2 * half) / V : 0);
+  const int half = tab.half, rotated = half / V, rest = copy_rest ? (head_dim - 2 * half) / V : 0, pieces = rotated + (rest + 1) / 2;
   const int places = n_here * pieces, head_lanes = places < kRopeThreads ? kRopeThreads / places : 1;
   for (int x = threadIdx.x; x < places * head_lanes; x += kRopeThreads) {
     const int hl = x / places, place = x - hl * places;
     const int k = place / pieces, j = place - k * pieces;
-    const bool turn = j < rotated;
-    // offsets of the two pieces; a piece that is copied has no second
-    int oa = j * V, ob = half + j * V;
-    if (tab.interleaved) {
-      oa = 2 * V * j;
-      ob = oa + V;
+    // Two pieces half the rotated part apart: of half layout both members of pairs Vj .., of neighbouring pairs (one
+    // channel at a time: the pair) V/2 pairs each.  Behind them: two that are copied (the last one twice if they are odd).
+    const bool turn = j < rotated, inside = V > 1 && tab.interleaved;
+    int oa = V == 1 && tab.interleaved ? 2 * j : V * j, ob = V == 1 && tab.interleaved ? oa + 1 : oa + half;
+    if (!turn) {
+      const int first = j - rotated, second = first + (rest + 1) / 2;
+      oa = 2 * half + V * first;
+      ob = 2 * half + V * (second < rest ? second : rest - 1);
     }
-    if (!turn) oa = ob = 2 * half + (j - rotated) * V;
     float c[V], s[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float2 f = turn ? cs[k][j * V + e] : make_float2(1.0f, 0.0f);
+      const float2 f = turn ? cs[k][!inside ? j * V + e : e < V / 2 ? j * V / 2 + e : half / 2 + j * V / 2 + e - V / 2] : make_float2(1.0f, 0.0f);
       c[e] = f.x;
       s[e] = f.y;
     }
@@ -105,36 +126,32 @@ __device__ __forceinline__ void rope_walk(const RopeTable &tab, const float2 (*c
         const T *from;
         to[u] = nullptr;
         if (h < n_heads && rows(k, h, from, to[u])) {
-          pa[u] = *reinterpret_cast<const P *>(from + oa);
-          if (turn) pb[u] = *reinterpret_cast<const P *>(from + ob);
+          pa[u] = piece_load<STREAM>(reinterpret_cast<const P *>(from + oa));
+          pb[u] = piece_load<STREAM>(reinterpret_cast<const P *>(from + ob));
         }
       }
 #pragma unroll
       for (int u = 0; u < kRopeAhead; ++u)
         if (to[u]) {
-          if (turn) {
-            P ra, rb;
-            if (V > 1 && tab.interleaved) {
+          P ra, rb;
+          if (inside) {
 #pragma unroll
-              for (int e = 0; e + 1 < V; e += 2) {  // (pairs within a piece)
-                const int f = e / 2, g = V / 2 + e / 2;
-                ra[e] = (T)rope_turned((float)pa[u][e], (float)pa[u][e + 1], c[f], -s[f]);
-                ra[e + 1] = (T)rope_turned((float)pa[u][e + 1], (float)pa[u][e], c[f], s[f]);
-                rb[e] = (T)rope_turned((float)pb[u][e], (float)pb[u][e + 1], c[g], -s[g]);
-                rb[e + 1] = (T)rope_turned((float)pb[u][e + 1], (float)pb[u][e], c[g], s[g]);
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < V; ++e) {
-                ra[e] = (T)rope_turned((float)pa[u][e], (float)pb[u][e], c[e], -s[e]);
-                rb[e] = (T)rope_turned((float)pb[u][e], (float)pa[u][e], c[e], s[e]);
-              }
+            for (int e = 0; e + 1 < V; e += 2) {  // (pairs within a piece)
+              const int f = e / 2, g = V / 2 + e / 2;
+              ra[e] = (T)rope_turned((float)pa[u][e], (float)pa[u][e + 1], c[f], -s[f]);
+              ra[e + 1] = (T)rope_turned((float)pa[u][e + 1], (float)pa[u][e], c[f], s[f]);
+              rb[e] = (T)rope_turned((float)pb[u][e], (float)pb[u][e + 1], c[g], -s[g]);
+              rb[e + 1] = (T)rope_turned((float)pb[u][e + 1], (float)pb[u][e], c[g], s[g]);
             }
-            *reinterpret_cast<P *>(to[u] + oa) = ra;
-            *reinterpret_cast<P *>(to[u] + ob) = rb;
           } else {
-            *reinterpret_cast<P *>(to[u] + oa) = pa[u];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              ra[e] = (T)rope_turned((float)pa[u][e], (float)pb[u][e], c[e], -s[e]);
+              rb[e] = (T)rope_turned((float)pb[u][e], (float)pa[u][e], c[e], s[e]);
+            }
           }
+          piece_store<STREAM>(reinterpret_cast<P *>(to[u] + oa), turn ? ra : pa[u]);
+          piece_store<STREAM>(reinterpret_cast<P *>(to[u] + ob), turn ? rb : pb[u]);
         }
     }
   }

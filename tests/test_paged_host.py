@@ -18,8 +18,8 @@ using namespace skvq;
 extern "C" int append_rows(int total, int n_new, int W, int S, int *out, int most) {
   const AppendPlan p = append_plan(total, n_new, W, S);
   int n = 0;
-  for (int u = 0; u < p.leaving_fours + p.vacant_fours; ++u)
-    for (int r = 0; r < 4; ++r) {
+  for (int u = 0; u < p.leaving + p.vacant; ++u)
+    for (int r = 0; r < 8; ++r) {
       const AppendRow x = append_row(p, u, r);
       if (!x.valid) continue;
       if (n == most) return -1;
@@ -30,12 +30,12 @@ extern "C" int append_rows(int total, int n_new, int W, int S, int *out, int mos
 }
 extern "C" int append_units(int total, int n_new, int W, int S) {
   const AppendPlan p = append_plan(total, n_new, W, S);
-  return p.leaving_fours + p.vacant_fours;
+  return p.leaving + p.vacant;
 }
 extern "C" long long start_of(int kind, int row0, int i) {
   return unit_start(kind == 0 ? kAppendDeal : kind == 1 ? kReadDeal : kTokenDeal, row0, i);
 }
-extern "C" int fours_to_read(int first, int n, int S) { return read_fours(first, n, S); }
+extern "C" int eights_to_read(int first, int n, int S) { return read_eights(first, n, S); }
 extern "C" int token_to_read(int first, int S, int unit, int r) { return read_token(first, S, unit, r); }
 extern "C" int place(int token, int total, int W, int S) {
   const TokenPlace p = token_place(token, total, W, S);
@@ -73,7 +73,7 @@ def B():
 
 
 def rows_of(plan, total, n_new, W, S):
-    out = np.zeros((4 * (n_new + 16), 8), np.int32)
+    out = np.zeros((8 * (n_new + 16), 8), np.int32)
     n = plan.append_rows(total, n_new, W, S, out.ctypes.data_as(C.c_void_p), len(out))
     assert n >= 0
     return out[:n]
@@ -90,7 +90,7 @@ def test_append_puts_every_token_in_its_place_once(plan, W, S):
             for u, r, leaving, old, token, te, fresh, row in rows_of(plan, total, n_new, W, S):
                 if leaving:
                     left.append(token)
-                    assert te == token - S and (te < 0 or te % 4 == r)        # the fours of a page
+                    assert te == token - S and (te < 0 or te % 8 == r)        # the eights of a page
                     assert old == (token < length)
                     if old:
                         assert row == token % W and ring[row] == token        # read where it is ...
@@ -113,7 +113,7 @@ def test_units_of_sequences_do_not_overlap(plan, W, S):
         for i, n in enumerate(news):
             extra = int(rng.choice([0, 1, W - 1, W, 2 * W + 3]))
             most = {0: plan.append_units(n + extra, n, W, S),
-                    1: max(plan.fours_to_read(extra, n, S), plan.fours_to_read(0, n, S)), 2: n}
+                    1: max(plan.eights_to_read(extra, n, S), plan.eights_to_read(0, n, S)), 2: n}
             for kind, units in most.items():
                 gap = plan.start_of(kind, int(row0[i + 1]), i + 1) - plan.start_of(kind, int(row0[i]), i)
                 assert units <= gap, (kind, n, extra)
@@ -123,9 +123,9 @@ def test_read_covers_its_tokens_once(plan):
     for S in (0, 1, 2, 3, 5):
         for first in range(0, 9):
             for n in range(0, 12):
-                got = [plan.token_to_read(first, S, u, r) for u in range(plan.fours_to_read(first, n, S)) for r in range(4)]
+                got = [plan.token_to_read(first, S, u, r) for u in range(plan.eights_to_read(first, n, S)) for r in range(8)]
                 assert [a for a in got if first <= a < first + n] == list(range(first, first + n))
-                assert len(got) <= 4 * (n // 4 + 2)
+                assert len(got) <= 8 * (n // 8 + 2)
     for total, W, S in [(5, 8, 2), (8, 8, 2), (9, 8, 2), (30, 8, 3), (30, 1, 0), (2 ** 31 - 65, 128, 5)]:
         for a in {0, 1, 2, 3, total // 2, max(total - W - 1, 0), max(total - W, 0), total - 1}:
             want = -1 - a % W if a >= total - W else -1 - (W + a) if a < S else a - S
