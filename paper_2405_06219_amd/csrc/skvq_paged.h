@@ -27,9 +27,9 @@ struct PagedLayout {
   uint8_t *pages;
   void *k_rows, *v_rows;
   float *workspace;
-  // device constants: channel of key code e of a row's dword m, at [head][8 m + e]; of value code n of piece
-  // m, at [head][8 m + n]; and the place 8 m + e of a key channel
-  const uint8_t *k_channel, *v_channel, *k_place;
+  // device constants: twice the channel (the offset of its 16-bit value) of key code e of a row's dword m, at
+  // [head][8 m + e]; of value code n of piece m, at [head][8 m + n]; and the place 8 m + e of a key channel
+  const uint8_t *k_offset, *v_offset, *k_place;
   const float *clip_k, *clip_v;  // [Hk][NG]
   int *errors;                   // SKVQ_PAGED_BAD_*
 };
@@ -80,6 +80,19 @@ __device__ __forceinline__ int sequence_of_unit(const PagedBatch &b, long long u
     n = n - k * step < step ? n - k * step : step;
   }
   return __builtin_amdgcn_readfirstlane(lo);
+}
+// The unit's sequence.  Up to 64 sequences: every lane reads one, all at once.
+__device__ __forceinline__ Sequence locate(const PagedBatch &b, const PagedLayout &L, long long unit, const UnitDeal &d, int &i) {
+  if (b.n_seqs > 64) {
+    i = sequence_of_unit(b, unit, d);
+    return sequence_of(b, L, i);
+  }
+  const int lane = threadIdx.x & 63;
+  Sequence s = sequence_of(b, L, lane < b.n_seqs ? lane : b.n_seqs - 1);
+  const unsigned long long started = __ballot(lane < b.n_seqs && unit_start(d, s.row0, lane) <= unit);
+  i = __builtin_amdgcn_readfirstlane(started ? 63 - __builtin_clzll(started) : 0);
+  auto of_it = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
+  return Sequence{of_it(s.row0), of_it(s.n_new), of_it(s.total), of_it(s.slot), (bool)of_it(s.counts_ok), (bool)of_it(s.slot_ok)};
 }
 inline long long units_of(const skvq_batch &b, const UnitDeal &d) {
   return (((long long)b.n_tokens * d.mul) >> d.div_log2) + (long long)b.n_seqs * d.pad;

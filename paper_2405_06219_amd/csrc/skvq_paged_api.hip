@@ -22,7 +22,7 @@ struct skvq_paged {
   int device = 0;
   int n_cus = 256;
   int max_tokens = 0;
-  void *dev_consts = nullptr;  // k_channel, v_channel, k_place, clip_k, clip_v, errors
+  void *dev_consts = nullptr;  // k_offset, v_offset, k_place, clip_k, clip_v, errors
   char last_error[256] = "";
 };
 
@@ -263,9 +263,10 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
     for (int m = 0; m < 16; ++m)
       for (int e = 0; e < 8; ++e) {
         const size_t at = (size_t)h * kD + 8 * m + e;
-        host[at] = (uint8_t)cfg->perm_k[(size_t)h * kD + 32 * (m & 3) + 8 * (m >> 2) + e];
-        host[off_p + (size_t)h * kD + host[at]] = (uint8_t)(8 * m + e);
-        host[off_v + at] = (uint8_t)cfg->perm_v[(size_t)h * kD + 16 * e + m];
+        const int channel = cfg->perm_k[(size_t)h * kD + 32 * (m & 3) + 8 * (m >> 2) + e];
+        host[at] = (uint8_t)(2 * channel);
+        host[off_p + (size_t)h * kD + channel] = (uint8_t)(8 * m + e);
+        host[off_v + at] = (uint8_t)(2 * cfg->perm_v[(size_t)h * kD + 16 * e + m]);
       }
   std::memcpy(&host[off_ck], cfg->clip_k, n_clip * 4);
   std::memcpy(&host[off_cv], cfg->clip_v, n_clip * 4);
@@ -276,8 +277,8 @@ int skvq_paged_create(const skvq_paged_config *cfg, const skvq_paged_buffers *bu
     return SKVQ_ERR_HIP;
   }
   uint8_t *d = (uint8_t *)c->dev_consts;
-  L.k_channel = d;
-  L.v_channel = d + off_v;
+  L.k_offset = d;
+  L.v_offset = d + off_v;
   L.k_place = d + off_p;
   L.clip_k = (const float *)(d + off_ck);
   L.clip_v = (const float *)(d + off_cv);

@@ -579,7 +579,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int h = blockIdx.x;  // (heads side by side: a head's units, row blocks of one chunk among them, share a chiplet's L2)
   const unsigned long long places = *reinterpret_cast<const unsigned long long *>(L.k_place + h * kD + 8 * c);
-  const int p = threadIdx.x % kD, packed_channel = L.v_channel[h * kD + 8 * (p & 15) + (p >> 4)];  // of the output place it writes
+  const int p = threadIdx.x % kD, packed_channel = L.v_offset[h * kD + 8 * (p & 15) + (p >> 4)] / 2;  // of the output place it writes
   const BatchPlan plan = plan_batch(L, b, gridDim.y, lds.members);
   __syncthreads();
   for (int unit = blockIdx.y; unit < plan.units; unit += gridDim.y) {

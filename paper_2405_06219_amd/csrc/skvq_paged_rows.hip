@@ -54,8 +54,8 @@ __device__ __forceinline__ void rotate_queries(const PagedLayout &L, const RopeT
     bool ok = token < b.n_tokens;
     int position = 0;
     if (ok) {
-      const int i = sequence_of_unit(b, token, kTokenDeal);
-      const Sequence s = sequence_of(b, L, i);
+      int i;
+      const Sequence s = locate(b, L, token, kTokenDeal, i);
       ok = s.counts_ok && s.slot_ok && token >= s.row0 && token < s.row0 + s.n_new;
       position = ok ? (b.positions ? b.positions[token] : s.total - s.n_new + token - s.row0) : 0;
     }
@@ -111,13 +111,13 @@ __device__ __forceinline__ void store_pieces(T *row, const LanePieces &at, const
   *reinterpret_cast<Piece<T, 8> *>(row + at.a) = x.a;
   *reinterpret_cast<Piece<T, 8> *>(row + at.b) = x.b;
 }
-// Rotates them.  c, s: cosines and sines of the lane's eight pairs (turns).  Rotated parts that do not fill pieces go
-// channel by channel through LDS (row: this row's place; cs: the row's cosines and sines).
-template <class T>
+// Rotates them.  WHOLE: the rotated part fills whole pieces, c and s are the cosines and sines of the lane's eight pairs
+// (of lanes that turns).  Else channel by channel through LDS (row: this row's place; cs: the row's cosines and sines).
+template <bool WHOLE, class T>
 __device__ __forceinline__ void rotate_pieces(const RopeTable &tab, const LanePieces &at, const float (&c)[8], const float (&s)[8],
                                               const float2 *cs, T *row, Pieces<T> &x) {
   const int half = tab.half;
-  if (half % 8 == 0) {
+  if constexpr (WHOLE) {
     if (!at.turns) return;
     Pieces<T> y;
     if (tab.interleaved) {
@@ -137,30 +137,35 @@ __device__ __forceinline__ void rotate_pieces(const RopeTable &tab, const LanePi
       }
     }
     x = y;
-    return;
-  }
-  store_pieces(row, at, x);
-  wave_lds_sync();
+  } else {
+    store_pieces(row, at, x);
+    wave_lds_sync();
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int ch = (e < 8 ? at.a : at.b - 8) + e;
-    if (ch < 2 * half) {
-      const bool first = tab.interleaved ? !(ch & 1) : ch < half;
-      const float2 f = cs[tab.interleaved ? ch >> 1 : first ? ch : ch - half];
-      const float other = (float)row[tab.interleaved ? ch ^ 1 : first ? ch + half : ch - half];
-      const float own = (float)(e < 8 ? x.a[e & 7] : x.b[e & 7]);
-      const T y = (T)rope_turned(own, other, f.x, first ? -f.y : f.y);
-      if (e < 8)
-        x.a[e & 7] = y;
-      else
-        x.b[e & 7] = y;
+    for (int e = 0; e < 16; ++e) {
+      const int ch = (e < 8 ? at.a : at.b - 8) + e;
+      if (ch < 2 * half) {
+        const bool first = tab.interleaved ? !(ch & 1) : ch < half;
+        const float2 f = cs[tab.interleaved ? ch >> 1 : first ? ch : ch - half];
+        const float other = (float)row[tab.interleaved ? ch ^ 1 : first ? ch + half : ch - half];
+        const float own = (float)(e < 8 ? x.a[e & 7] : x.b[e & 7]);
+        const T y = (T)rope_turned(own, other, f.x, first ? -f.y : f.y);
+        if (e < 8)
+          x.a[e & 7] = y;
+        else
+          x.b[e & 7] = y;
+      }
     }
+    wave_lds_sync();
   }
-  wave_lds_sync();
 }
 
 __device__ __forceinline__ unsigned long long lane_bytes(const uint8_t *p) { return *reinterpret_cast<const unsigned long long *>(p); }
-__device__ __forceinline__ int byte_of(unsigned long long w, int e) { return (int)((w >> (8 * e)) & 0xffu); }
+// The value of a parked row at the e-th of eight byte offsets.
+template <class T>
+__device__ __forceinline__ T &at_offset(T *row, unsigned long long offsets, int e) {
+  const unsigned half = e < 4 ? (unsigned)offsets : (unsigned)(offsets >> 32);
+  return *reinterpret_cast<T *>(reinterpret_cast<char *>(row) + ((half >> (8 * (e & 3))) & 0xffu));
+}
 // The element of a dword of key codes in nibble n: (0, 2, 4, 6, 1, 3, 5, 7).
 constexpr int key_element(int n) { return n < 4 ? 2 * n : 2 * n - 7; }
 // A lane's two dwords of a key row, and its two value pieces.
@@ -177,16 +182,16 @@ __device__ __forceinline__ unsigned code_in_low_bits(float x, const GroupParams 
 }
 
 // Quantizes an eight's key rows of one head (parked in LDS) and stores codes and pairs.  part: the head's part
-// of the page, or null; rp: the row's place in it.  channels: those of the lane's two dwords.
+// of the page, or null; rp: the row's place in it.  offsets: of the channels of the lane's two dwords.
 template <class T, int NG>
-__device__ __forceinline__ void pack_keys(const PagedLayout &L, const T *row, const unsigned long long (&channels)[2], const float *clip,
+__device__ __forceinline__ void pack_keys(const PagedLayout &L, T *row, const unsigned long long (&offsets)[2], const float *clip,
                                           uint8_t *part, int rp, int m) {
   float x[2][8], mn, mx;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      x[i][e] = (float)row[byte_of(channels[i], e)];
+      x[i][e] = (float)at_offset(row, offsets[i], e);
       mn = i + e ? fminf(mn, x[i][e]) : x[i][e];
       mx = i + e ? fmaxf(mx, x[i][e]) : x[i][e];
     }
@@ -210,7 +215,7 @@ __device__ __forceinline__ void pack_keys(const PagedLayout &L, const T *row, co
 
 // ... its value rows: the lane's pieces hold positions 16n + piece, n = 0 .. 7, some of every group.
 template <class T, int NG>
-__device__ __forceinline__ void pack_values(const PagedLayout &L, const T *row, const unsigned long long (&channels)[2], const float *clip,
+__device__ __forceinline__ void pack_values(const PagedLayout &L, T *row, const unsigned long long (&offsets)[2], const float *clip,
                                             uint8_t *part, int rp, int m) {
   unsigned w[2] = {0u, 0u};
 #pragma unroll
@@ -220,7 +225,7 @@ __device__ __forceinline__ void pack_values(const PagedLayout &L, const T *row, 
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < 8 / NG; ++e) {
-        x[i][e] = (float)row[byte_of(channels[i], g * (8 / NG) + e)];
+        x[i][e] = (float)at_offset(row, offsets[i], g * (8 / NG) + e);
         mn = i + e ? fminf(mn, x[i][e]) : x[i][e];
         mx = i + e ? fmaxf(mx, x[i][e]) : x[i][e];
       }
@@ -253,20 +258,21 @@ __device__ __forceinline__ void pack_values(const PagedLayout &L, const T *row, 
   }
 }
 
-// Append: see AppendPlan for which lanes do what.
-template <class T, int NG>
+// Append: see AppendPlan for which lanes do what.  WHOLE: see rotate_pieces.  QUERIES: workgroups from n_units on rotate
+// the queries.
+template <class T, int NG, bool WHOLE, bool QUERIES>
 __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedLayout L, const RopeTable tab, const PagedBatch b,
                                                                     const TokenRows k, const TokenRows v, const QueryRows q,
                                                                     unsigned n_units, int heads_per_group) {
   __shared__ float2 cs[kEight][kRopeMaxPairs / 2];  // (a head of 128 channels has 64 pairs)
   __shared__ __align__(16) T parked[4][kEight][kRowStride];
-  if (blockIdx.x >= n_units) {
+  if (QUERIES && blockIdx.x >= n_units) {
     static_assert(sizeof cs >= sizeof(float2[kRopeMaxTokens][kRopeMaxPairs]), "queries use it with a stride of their own");
     if (blockIdx.y == 0) rotate_queries<T>(L, tab, b, q, blockIdx.x - n_units, reinterpret_cast<float2(*)[kRopeMaxPairs]>(cs));
     return;
   }
-  const int i = sequence_of_unit(b, blockIdx.x, kAppendDeal);
-  const Sequence s = sequence_of(b, L, i);
+  int i;
+  const Sequence s = locate(b, L, blockIdx.x, kAppendDeal, i);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 3, m = lane & 7;
   const long long unit = blockIdx.x - unit_start(kAppendDeal, s.row0, i);
   if (!s.counts_ok || !s.slot_ok) {
@@ -287,12 +293,14 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedL
   __syncthreads();
   const bool keys = wave < 2;  // wavefronts 0, 1: keys; 2, 3: values
   const LanePieces at = lane_pieces(tab, m);
-  float c[8], sn[8];
+  float c[8] = {}, sn[8] = {};
+  if (WHOLE && keys && at.turns) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 f = keys && at.turns ? cs[r][8 * m + e] : make_float2(1.0f, 0.0f);
-    c[e] = f.x;
-    sn[e] = f.y;
+    for (int e = 0; e < 8; ++e) {
+      const float2 f = cs[r][8 * m + e];
+      c[e] = f.x;
+      sn[e] = f.y;
+    }
   }
   const TokenRows src = keys ? k : v;
   T *rows = reinterpret_cast<T *>(keys ? L.k_rows : L.v_rows) + (long long)s.slot * L.Hk * (L.W + L.S) * kD;
@@ -300,15 +308,15 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedL
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
     T *head_rows = rows + (long long)h * (L.W + L.S) * kD;
-    const uint8_t *order = (keys ? L.k_channel : L.v_channel) + h * kD;
-    const unsigned long long channels[2] = {lane_bytes(order + 8 * (keys ? key_dword(m, 0) : value_piece(m, 0))),
-                                            lane_bytes(order + 8 * (keys ? key_dword(m, 1) : value_piece(m, 1)))};
+    const uint8_t *order = (keys ? L.k_offset : L.v_offset) + h * kD;
+    const unsigned long long offsets[2] = {lane_bytes(order + 8 * (keys ? key_dword(m, 0) : value_piece(m, 0))),
+                                           lane_bytes(order + 8 * (keys ? key_dword(m, 1) : value_piece(m, 1)))};
     Pieces<T> fresh = {}, gone = {};
     if (x.valid) {
       fresh = load_pieces((const T *)src.p + token * src.stride + h * kD, at);
       if (x.old) gone = load_pieces(head_rows + (long long)x.ring * kD, at);
     }
-    if (keys && tab.half) rotate_pieces(tab, at, c, sn, cs[r], row, fresh);
+    if (keys && tab.half) rotate_pieces<WHOLE>(tab, at, c, sn, cs[r], row, fresh);
     if (x.valid && x.ring >= 0) store_pieces(head_rows + (long long)x.ring * kD, at, fresh);
     if (!x.leaving) continue;
     if (!x.old) gone = fresh;
@@ -318,26 +326,49 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_kernel(const PagedL
     uint8_t *part = page ? page + (long long)h * L.part_bytes : nullptr;
     const int rp = x.te & ((1 << L.page_log2) - 1);
     if (keys)
-      pack_keys<T, NG>(L, row, channels, L.clip_k + h * NG, part, rp, m);
+      pack_keys<T, NG>(L, row, offsets, L.clip_k + h * NG, part, rp, m);
     else
-      pack_values<T, NG>(L, row, channels, L.clip_v + h * NG, part, rp, m);
+      pack_values<T, NG>(L, row, offsets, L.clip_v + h * NG, part, rp, m);
     wave_lds_sync();
   }
 }
 
-// scale * code + zero, each operation rounded once
-__device__ __forceinline__ float dequantized(unsigned code, float2 pair) {
+// The queries of a large batch by themselves (their walk needs more registers than an eight of keys and values).
+template <class T>
+__global__ __launch_bounds__(kRopeThreads) void paged_queries_kernel(const PagedLayout L, const RopeTable tab, const PagedBatch b, const QueryRows q) {
+  __shared__ float2 cs[kRopeMaxTokens][kRopeMaxPairs];
+  rotate_queries<T>(L, tab, b, q, blockIdx.x, cs);
+}
+
+// scale * code + zero, each operation rounded once.  EXACT: the product is (a compact scale has at most 11 bits, a code
+// four), and one multiply-add gives the same number.
+template <bool EXACT>
+__device__ __forceinline__ float dequantized(float code, float2 pair) {
 #pragma clang fp contract(off)
-  const float p = pair.x * (float)code;
-  return p + pair.y;
+  if constexpr (EXACT) {
+    return __builtin_fmaf(pair.x, code, pair.y);
+  } else {
+    const float p = pair.x * code;
+    return p + pair.y;
+  }
+}
+// Eight codes of a dword into a parked row at their offsets; element(n): which of them nibble n is, and its pair.
+template <bool EXACT, class T, class Element, class Pair>
+__device__ __forceinline__ void scatter_codes(unsigned w, T *row, unsigned long long offsets, Element element, Pair pair) {
+  const unsigned even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    const float code = (float)(((n % 2 ? odd : even) >> (8 * (n / 2))) & 0xffu);
+    at_offset(row, offsets, element(n)) = (T)dequantized<EXACT>(code, pair(n));
+  }
 }
 
 template <class T, int NG>
 __global__ __launch_bounds__(kRopeThreads) void paged_read_kernel(const PagedLayout L, const PagedBatch b, T *k, long long k_stride,
                                                                   T *v, long long v_stride, int heads_per_group) {
   __shared__ __align__(16) T parked[4][kEight][kRowStride];
-  const int i = sequence_of_unit(b, blockIdx.x, kReadDeal);
-  const Sequence s = sequence_of(b, L, i);
+  int i;
+  const Sequence s = locate(b, L, blockIdx.x, kReadDeal, i);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane >> 3, m = lane & 7;
   const long long unit = blockIdx.x - unit_start(kReadDeal, s.row0, i);
   const int f = b.first ? b.first[i] : s.total - s.n_new;
@@ -366,34 +397,41 @@ __global__ __launch_bounds__(kRopeThreads) void paged_read_kernel(const PagedLay
   T *row = parked[wave][r];
   const LanePieces at = {8 * m, kD / 2 + 8 * m, false};  // (whole lines per instruction)
   const int h1 = min(L.Hk, (int)(blockIdx.y + 1) * heads_per_group);
+  const bool exact = L.meta_fmt != SKVQ_META_F32;
   for (int h = blockIdx.y * heads_per_group + (wave & 1); h < h1; h += 2) {
     Pieces<T> x = {};
     if (valid && full) x = load_pieces(rows + ((long long)h * (L.W + L.S) + place.row) * kD, at);
     if (valid && !full) {
-      const uint8_t *part = page + (long long)h * L.part_bytes, *order = (keys ? L.k_channel : L.v_channel) + h * kD;
+      const uint8_t *part = page + (long long)h * L.part_bytes, *order = (keys ? L.k_offset : L.v_offset) + h * kD;
+      unsigned w[2];
+      unsigned long long offsets[2];
+      float2 pair[NG];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int e = 0; e < 2; ++e) {
+        const int dword = keys ? key_dword(m, e) : value_piece(m, e);
+        offsets[e] = lane_bytes(order + 8 * dword);
         if (keys) {
-          const unsigned w = reinterpret_cast<const unsigned *>(part + rp * (kD / 2))[key_dword(m, i)];
-          const unsigned long long ch = lane_bytes(order + 8 * key_dword(m, i));
-          const float2 pair = meta_load_pair(part + L.km_at, rp * NG + (m >> 1) * NG / 4, L.meta_fmt);
-#pragma unroll
-          for (int n = 0; n < 8; ++n) row[byte_of(ch, key_element(n))] = (T)dequantized((w >> (4 * n)) & 15u, pair);
-        } else {
-          // the row's halves of two dwords
-          const uint2 two = *reinterpret_cast<const uint2 *>(part + L.v_at + (rp >> 2) * (2 * kD) + 16 * value_piece(m, i) + 8 * ((rp & 3) >> 1));
-          const unsigned w = __builtin_amdgcn_perm(two.y, two.x, rp & 1 ? 0x07060302u : 0x05040100u);
-          const unsigned long long ch = lane_bytes(order + 8 * value_piece(m, i));
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const float2 pair = meta_load_pair(part + L.vm_at, rp * NG + g, L.meta_fmt);
-#pragma unroll
-            for (int e = 0; e < 8 / NG; ++e) {
-              const int n = g * (8 / NG) + e;
-              row[byte_of(ch, n)] = (T)dequantized((w >> (4 * n)) & 15u, pair);
-            }
-          }
+          w[e] = reinterpret_cast<const unsigned *>(part + rp * (kD / 2))[dword];
+        } else {  // the row's halves of two dwords
+          const uint2 two = *reinterpret_cast<const uint2 *>(part + L.v_at + (rp >> 2) * (2 * kD) + 16 * dword + 8 * ((rp & 3) >> 1));
+          w[e] = __builtin_amdgcn_perm(two.y, two.x, rp & 1 ? 0x07060302u : 0x05040100u);
         }
+      }
+      if (keys) {
+        pair[0] = meta_load_pair(part + L.km_at, rp * NG + (m >> 1) * NG / 4, L.meta_fmt);
+      } else {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) pair[g] = meta_load_pair(part + L.vm_at, rp * NG + g, L.meta_fmt);
+      }
+      auto key_pair = [&](int) { return pair[0]; };
+      auto value_pair = [&](int n) { return pair[n * NG / 8]; };
+      auto same = [](int n) { return n; };
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (keys && exact) scatter_codes<true>(w[e], row, offsets[e], key_element, key_pair);
+        if (keys && !exact) scatter_codes<false>(w[e], row, offsets[e], key_element, key_pair);
+        if (!keys && exact) scatter_codes<true>(w[e], row, offsets[e], same, value_pair);
+        if (!keys && !exact) scatter_codes<false>(w[e], row, offsets[e], same, value_pair);
       }
     }
     wave_lds_sync();
@@ -411,15 +449,32 @@ int heads_per_group(int Hk, long long units, int n_cus) {
   return n;
 }
 
+template <class T, bool WHOLE, bool QUERIES>
+void launch_append_as(const PagedLayout &L, const RopeTable &tab, const PagedBatch &b, TokenRows k, TokenRows v, QueryRows q, unsigned units,
+                      dim3 grid, int heads, hipStream_t s) {
+  switch (L.NG) {
+    case 1: paged_append_kernel<T, 1, WHOLE, QUERIES><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
+    case 2: paged_append_kernel<T, 2, WHOLE, QUERIES><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
+    default: paged_append_kernel<T, 4, WHOLE, QUERIES><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
+  }
+}
 template <class T>
 hipError_t launch_append(const PagedLayout &L, const RopeTable &tab, const PagedBatch &b, TokenRows k, TokenRows v, QueryRows q,
                          unsigned units, unsigned query_groups, int heads, hipStream_t s) {
-  const dim3 grid(units + query_groups, (L.Hk + heads - 1) / heads);
-  switch (L.NG) {
-    case 1: paged_append_kernel<T, 1><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
-    case 2: paged_append_kernel<T, 2><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
-    default: paged_append_kernel<T, 4><<<grid, kRopeThreads, 0, s>>>(L, tab, b, k, v, q, units, heads); break;
+  // One launch for both while a launch is much of the call; large batches take two (25143 tokens of 32 query and 8 kv heads
+  // 147 us in one launch, 128 in two).
+  const bool apart = query_groups && b.n_tokens >= 2048;
+  if (apart) {
+    paged_queries_kernel<T><<<query_groups, kRopeThreads, 0, s>>>(L, tab, b, q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
+  const bool queries = query_groups && !apart;
+  const dim3 grid(units + (queries ? query_groups : 0), (L.Hk + heads - 1) / heads);
+  if (tab.half % 8 == 0)
+    queries ? launch_append_as<T, true, true>(L, tab, b, k, v, q, units, grid, heads, s) : launch_append_as<T, true, false>(L, tab, b, k, v, q, units, grid, heads, s);
+  else
+    queries ? launch_append_as<T, false, true>(L, tab, b, k, v, q, units, grid, heads, s) : launch_append_as<T, false, false>(L, tab, b, k, v, q, units, grid, heads, s);
   return hipGetLastError();
 }
 
