@@ -184,12 +184,14 @@ __device__ __forceinline__ Member member_in_lane(const PagedLayout &L, const Pag
   m.c = chunks_of(m.s.counts_ok ? m.s.total : 1, L.W, L.S, chunk);
   return m;
 }
-// What a workgroup needs to know of the batch.  (Units are counted in 32 bits: the host refuses a call that could have
-// more.)  The first 64 sequences are kept in LDS, written by the first wavefront.
+// What a workgroup needs to know of the batch: first come the units of packed rows, sequence by sequence, then those of
+// full rows.  (Units are counted in 32 bits: the host refuses a call that could have more.)  The first 64 sequences are
+// kept in LDS, written by the first wavefront.
 struct BatchPlan {
-  int chunk, units;  // chunk size; units per kv head
-  int upto;          // units of the sequences up to number `lane`
+  int chunk, packed_units, units;  // chunk size; units per kv head
+  int packed_upto, rows_upto;      // units of the sequences up to number `lane`
 };
+__device__ __forceinline__ int units_in_lane(const Member &m, bool packed) { return m.blocks * (packed ? m.c.packed : m.c.rows); }
 __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const PagedBatch &b, int groups, Member (&members)[64]) {
   const int lane = threadIdx.x & 63;
   BatchPlan p;
@@ -200,7 +202,7 @@ __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const Page
   for (int i0 = 0;;) {
     bad = bad || !m.s.counts_ok;
     work += (float)m.blocks * m.c.nq;
-    extra += (float)m.blocks * (m.c.rows + (m.c.nq > 0));
+    extra += (float)m.blocks * (m.c.nq > 0);
     if ((i0 += 64) >= b.n_seqs) break;
     m = member_in_lane(L, b, i0 + lane, kPagedMinChunk);
   }
@@ -208,25 +210,31 @@ __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const Page
   p.chunk = uniform(chunk_for(last_lane(lanes_up_to(work)), last_lane(lanes_up_to(extra)), groups));
   if (p.chunk != kPagedMinChunk) mine.c = chunks_of(mine.s.counts_ok ? mine.s.total : 1, L.W, L.S, p.chunk);
   if (threadIdx.x < 64) members[lane] = mine;
-  p.upto = lanes_up_to(mine.blocks * (mine.c.rows + mine.c.packed));
-  p.units = last_lane(p.upto);
+  p.packed_upto = lanes_up_to(units_in_lane(mine, true));
+  p.rows_upto = lanes_up_to(units_in_lane(mine, false));
+  p.packed_units = last_lane(p.packed_upto);
+  p.units = last_lane(p.rows_upto);
   for (int i0 = 64; i0 < b.n_seqs; i0 += 64) {
     m = member_in_lane(L, b, i0 + lane, p.chunk);
-    p.units += last_lane(lanes_up_to(m.blocks * (m.c.rows + m.c.packed)));
+    p.packed_units += last_lane(lanes_up_to(units_in_lane(m, true)));
+    p.units += last_lane(lanes_up_to(units_in_lane(m, false)));
   }
+  p.units += p.packed_units;
   return p;
 }
-// The unit's sequence with its chunks, its rows, its chunk.  A chunk's row blocks are neighbours: they read the same rows.
+// The unit's sequence with its chunks, its rows, its chunk (of packed or of full rows).  A chunk's row blocks are
+// neighbours: they read the same rows.
 __device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, const Member (&members)[64],
-                                              int unit, Chunks &c, int &chunk) {
+                                              int unit, Chunks &c, int &chunk, bool &packed) {
   const int lane = threadIdx.x & 63;
   RowBlock x;
-  int i0 = 0, upto = p.upto;
-  while (last_lane(upto) <= unit && i0 + 64 < b.n_seqs) {  // (unit < p.units)
+  packed = unit < p.packed_units;
+  if (!packed) unit -= p.packed_units;
+  int i0 = 0, upto = packed ? p.packed_upto : p.rows_upto;
+  while (last_lane(upto) <= unit && i0 + 64 < b.n_seqs) {  // (the unit is one of those counted)
     unit -= last_lane(upto);
     i0 += 64;
-    const Member m = member_in_lane(L, b, i0 + lane, p.chunk);
-    upto = lanes_up_to(m.blocks * (m.c.rows + m.c.packed));
+    upto = lanes_up_to(units_in_lane(member_in_lane(L, b, i0 + lane, p.chunk), packed));
   }
   const unsigned long long behind = __ballot(upto > unit);
   const int k = uniform(behind ? __ffsll(behind) - 1 : 63);
@@ -584,9 +592,9 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
   __syncthreads();
   for (int unit = blockIdx.y; unit < plan.units; unit += gridDim.y) {
     int chunk;
+    bool packed;
     Chunks ch;
-    const RowBlock x = find_unit(L, b, plan, lds.members, unit, ch, chunk);
-    const bool packed = chunk >= ch.rows;
+    const RowBlock x = find_unit(L, b, plan, lds.members, unit, ch, chunk, packed);
     // the queries, sixteen threads a row, rows past the last one repeat it; the first pages meanwhile
     static_assert(64 * kWaves == 16 * 16, "one piece of a row per thread");
     const int query = threadIdx.x >> 4;
@@ -595,7 +603,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
     bool bad = false;
     int ids = 0;
     if (packed) {
-      const int begin = (chunk - ch.rows) * ch.chunk;
+      const int begin = chunk * ch.chunk;
       ids = pages_of_tiles(L, b, x.i, begin, min(ch.nq, begin + ch.chunk), 0, bad);
     }
     __syncthreads();  // (the unit before has read its partials out of LDS)
@@ -613,7 +621,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
     State<NG> st;
     st.clear();
     if (packed)
-      take_packed<T, NG, FMT>(L, b, lds, x, ch, chunk - ch.rows, h, ids, st, bad);
+      take_packed<T, NG, FMT>(L, b, lds, x, ch, chunk, h, ids, st, bad);
     else if (x.s.slot_ok)
       take_rows<T, NG>(L, lds, x, ch, chunk, h, st);
 
@@ -669,14 +677,14 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
       if (n_partials == 1) {
         store_out<T>(L, out, qr, channel, acc / l);
       } else {
-        float *part = to + chunk * kPartialStride;
+        float *part = to + (packed ? ch.rows + chunk : chunk) * kPartialStride;
         part[4 + channel] = acc;
         if (p == 0) {
           part[0] = m;
           part[1] = l;
         }
       }
-      if (p == 0 && chunk == 0) to[2] = __uint_as_float((unsigned)n_partials);  // (for the merge)
+      if (p == 0 && !packed && chunk == 0) to[2] = __uint_as_float((unsigned)n_partials);  // (for the merge)
     }
   }
 }

@@ -91,10 +91,10 @@ constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
 constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
 constexpr int whole_steps(int rows) { return (rows / kPagedStep + (rows % kPagedStep > 0)) * kPagedStep; }
 // Lengths are known on the device only, so every workgroup, of `groups` per kv head, finds the batch's chunk size from two
-// sums over the batch: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a
-// chunk of full rows and a last, shorter chunk of packed ones per block).  The units fit `rounds` rounds over the
-// groups of a head: as few as keep a chunk within 4096 rows, more where the extra units would fill half of them.
-// (Numbers of 24 bits do: the units are counted exactly from the chunk size, which is the same in every workgroup.)
+// sums over the batch: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a last, shorter
+// chunk per block).  The units of packed rows fit `rounds` rounds over the groups of a head: as few as keep a chunk within
+// 4096 rows, more where the extra units would fill half of them.  (The units of full rows, short ones, come after them.
+// Numbers of 24 bits do: units are counted exactly from the chunk size, which is the same in every workgroup.)
 constexpr int chunk_for(float work, float extra, int groups) {
   const float least = work / (4096.0f * groups), full = 2.0f * extra / groups;
   const float most = least > full ? least : full;

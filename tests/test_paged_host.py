@@ -146,7 +146,7 @@ def test_chunks_cover_all_rows(plan):
 
 @pytest.mark.parametrize("groups", [1, 24, 96, 768])
 def test_units_fill_rounds_of_the_workgroups(plan, groups):
-    """The chunk size that the device finds: the batch's units fit whole rounds over the workgroups."""
+    """The chunk size that the device finds: the batch's units of packed rows fit whole rounds over the workgroups."""
     rng = np.random.default_rng(groups)
     out = np.zeros(6, np.int32)
     plan.chunk_size.argtypes = [C.c_float, C.c_float, C.c_int]
@@ -160,11 +160,11 @@ def test_units_fill_rounds_of_the_workgroups(plan, groups):
             return [int(x) for x in out]
         got = [chunks(t, 256) for t in lens]
         work = sum(b * c[2] for b, c in zip(blocks, got))
-        extra = sum(b * (c[3] + (c[2] > 0)) for b, c in zip(blocks, got))
+        extra = sum(b * (c[2] > 0) for b, c in zip(blocks, got))
         size = plan.chunk_size(work, extra, groups)
         assert size % 128 == 0 and size >= 256
         rounds = max(work / (4096 * groups), 2 * extra / groups) * (1 + 1e-6) // 1 + 1
-        units = sum(b * (c[3] + c[4]) for b, c in zip(blocks, [chunks(t, size) for t in lens]))
+        units = sum(b * c[4] for b, c in zip(blocks, [chunks(t, size) for t in lens]))
         assert units <= rounds * groups
     assert plan.chunk_size(0, 0, groups) == 256
     assert plan.chunk_size(2.0 ** 62, 2.0 ** 40, groups) >= 256
