@@ -1,6 +1,6 @@
 // skvq_paged_attention: the batch's query tokens over pages of 4-bit rows and the fp16 / bf16 rows (Eq. 1).
 //
-// A workgroup of four wavefronts takes one chunk of one sequence's tokens for one kv head and up to sixteen
+// A workgroup of four wavefronts takes one chunk of one sequence's tokens for one kv head and RB blocks of sixteen
 // (query token, query head) rows; a wavefront takes every fourth tile of 32 tokens:
 //   scores  S^T[token][row] = K Q^T by v_mfma_f32_16x16x32_f16, two blocks of 16 tokens.  The A operand is the
 //           lane's 16 bytes of a key row: (w << 4, w, w >> 4, w >> 8) & 0x00f000f0 are its eight codes as fp16
@@ -13,8 +13,11 @@
 //           leaves S^T (lane: row lane % 16, tokens 4 (lane / 16) + 0..3 of both blocks), and a lane's 16 bytes of
 //           four value rows are the A operand's tokens of eight positions: nothing crosses lanes in the loop.
 // The (scale, zero) pairs of a lane's eight tokens, of keys and values, sit in the lanes of its row of 16 (PairSlot): one
-// load, conversion and logarithm per tile and group, and every use reads them by a lane broadcast that is part of the
-// instruction.
+// load, conversion and logarithm per tile and group, and every use reads them by a lane broadcast.  What a tile's pairs, key
+// codes and value codes leave free, the next tile's take in the same registers (a second buffer is 26 registers at four
+// groups and hides no more: HBM answers within half a tile's work).
+// Work on vectors bounds calls of many rows per kv head: two blocks share unpacking and broadcasts (RB = 2), which takes
+// eight sequences of up to 40k tokens with two to eight new ones, four fp32 groups, from 119 to 115 us.
 //
 // The weight that multiplies a code is weight * scale: the reference counts log2 of the largest scale at hand in, so
 // that this product, rounded to fp16 (half a step of 2^-10; a second part as in the fixed cache's kernel would refine
@@ -35,14 +38,16 @@ namespace skvq {
 namespace {
 
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef unsigned uint4_t __attribute__((ext_vector_type(4)));
 typedef unsigned uint2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = kPagedWaves, kTile = kPagedTile;
-// workgroups that a compute unit holds: a third set of registers does not fit four accumulators per score
-constexpr int groups_per_cu(int NG) { return NG == 4 ? 2 : 3; }
+// workgroups that a compute unit holds: a third set of registers does not fit four accumulators per score, or the state
+// of two blocks of query rows
+constexpr int groups_per_cu(int NG, int RB) { return NG == 4 || RB > 1 ? 2 : 3; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kCodeUnit = 1048576.0f;      // 2^20: a code is the fp16 number code * 2^-20
 constexpr float kWeightShift = 10.0f;        // a row's largest weight is 2^10 when its reference moves ...
@@ -54,6 +59,7 @@ constexpr int kRowStride = kD + 4;           // floats per parked accumulator ro
 
 __device__ __forceinline__ float4_t mfma(half8_t a, half8_t b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float4_t mfma(bf8_t a, bf8_t b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ half8_t as_half8(unsigned a, unsigned b, unsigned c, unsigned d) {
   return __builtin_bit_cast(half8_t, uint4_t{a, b, c, d});
 }
@@ -70,6 +76,13 @@ __device__ __forceinline__ void unrolled(F f) {  // f(I) .. f(N - 1), the number
 template <int X>
 __device__ __forceinline__ float of_lane(float v) {
   return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + X, 0xF, 0xF, true));
+}
+
+// The row of 16 lanes turned so that lane X's value comes to lane 0.
+template <int X>
+__device__ __forceinline__ float from_lane(float v) {
+  if (X == 0) return v;
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + (16 - X) % 16, 0xF, 0xF, true));
 }
 
 // The largest of the row's 16 lanes, in all of them.
@@ -93,7 +106,6 @@ struct PairWord {
     if constexpr (FMT == SKVQ_META_F32) {
       return make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
     } else if constexpr (FMT == SKVQ_META_F16) {
-      typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
       const half2_t h = __builtin_bit_cast(half2_t, w);
       return make_float2((float)h[0], (float)h[1]);
     } else {
@@ -102,11 +114,28 @@ struct PairWord {
   }
 };
 
+template <int FMT>
+struct ZeroWord {  // a pair's zero
+  typename std::conditional<FMT == SKVQ_META_F32, float, typename std::conditional<FMT == SKVQ_META_F16, _Float16, uint8_t>::type>::type w;
+  __device__ __forceinline__ void load(const uint8_t *p) { w = *reinterpret_cast<const decltype(w) *>(p + sizeof(w)); }
+  __device__ __forceinline__ float value() const {
+    if constexpr (FMT == SKVQ_META_FP8_E4M3)
+      return __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+    else
+      return (float)w;
+  }
+};
+
+// Zeros enter scores and outputs by products with the queries' sums and with the weights.  Of four groups, these are fp32
+// matrix instructions: 4 multiplications a lane and score, each with a broadcast before it, would be a quarter of the work.
+constexpr bool zeros_by_matrix(int NG) { return NG == 4; }
+
 // A tile's packed data as a lane holds it.
 template <int NG, int FMT>
 struct Tile {
   uint4_t k[2], v[2];
   PairWord<FMT> pairs[NG];
+  ZeroWord<FMT> k_zero[zeros_by_matrix(NG) ? 2 : 1];  // of key row c, group g of either block
 };
 
 // Which pair lane c of a row of 16 holds in pairs[q]: 16 NG pairs in the order [keys, values][block][token of four][group].
@@ -127,7 +156,7 @@ struct Out {
   float *f32;
 };
 
-// A unit's rows: up to 16 (query token, query head) rows of a kv head of one sequence.
+// A unit's rows: up to RB blocks of 16 (query token, query head) rows of a kv head of one sequence.
 struct RowBlock {
   int i;      // sequence
   Sequence s;
@@ -170,16 +199,17 @@ __device__ __forceinline__ V last_lane(V x) {
   return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// A sequence of the batch with its chunks, and `blocks` blocks of 16 query rows (none where its counts are bad).
+// A sequence of the batch with its chunks, and `blocks` units' worth of query rows (none where its counts are bad).
 struct Member {
   Sequence s;
   Chunks c;
   int blocks;
 };
+template <int RB>
 __device__ __forceinline__ Member member_in_lane(const PagedLayout &L, const PagedBatch &b, int i, int chunk) {
   Member m;
   m.s = sequence_of(b, L, i < b.n_seqs ? i : b.n_seqs - 1);
-  m.blocks = i < b.n_seqs && m.s.counts_ok ? (m.s.n_new * L.R + 15) >> 4 : 0;
+  m.blocks = i < b.n_seqs && m.s.counts_ok ? (m.s.n_new * L.R + 16 * RB - 1) / (16 * RB) : 0;
   if (i >= b.n_seqs) m.s.counts_ok = true;
   m.c = chunks_of(m.s.counts_ok ? m.s.total : 1, L.W, L.S, chunk);
   return m;
@@ -192,10 +222,11 @@ struct BatchPlan {
   int packed_upto, rows_upto;      // units of the sequences up to number `lane`
 };
 __device__ __forceinline__ int units_in_lane(const Member &m, bool packed) { return m.blocks * (packed ? m.c.packed : m.c.rows); }
+template <int RB>
 __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const PagedBatch &b, int groups, Member (&members)[64]) {
   const int lane = threadIdx.x & 63;
   BatchPlan p;
-  Member mine = member_in_lane(L, b, lane, kPagedMinChunk);
+  Member mine = member_in_lane<RB>(L, b, lane, kPagedMinChunk);
   float work = 0.0f, extra = 0.0f;
   bool bad = false;
   Member m = mine;
@@ -204,7 +235,7 @@ __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const Page
     work += (float)m.blocks * m.c.nq;
     extra += (float)m.blocks * (m.c.nq > 0);
     if ((i0 += 64) >= b.n_seqs) break;
-    m = member_in_lane(L, b, i0 + lane, kPagedMinChunk);
+    m = member_in_lane<RB>(L, b, i0 + lane, kPagedMinChunk);
   }
   if (bad && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(L.errors, SKVQ_PAGED_BAD_COUNTS);
   p.chunk = uniform(chunk_for(last_lane(lanes_up_to(work)), last_lane(lanes_up_to(extra)), groups));
@@ -215,7 +246,7 @@ __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const Page
   p.packed_units = last_lane(p.packed_upto);
   p.units = last_lane(p.rows_upto);
   for (int i0 = 64; i0 < b.n_seqs; i0 += 64) {
-    m = member_in_lane(L, b, i0 + lane, p.chunk);
+    m = member_in_lane<RB>(L, b, i0 + lane, p.chunk);
     p.packed_units += last_lane(lanes_up_to(units_in_lane(m, true)));
     p.units += last_lane(lanes_up_to(units_in_lane(m, false)));
   }
@@ -224,6 +255,7 @@ __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const Page
 }
 // The unit's sequence with its chunks, its rows, its chunk (of packed or of full rows).  A chunk's row blocks are
 // neighbours: they read the same rows.
+template <int RB>
 __device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, const Member (&members)[64],
                                               int unit, Chunks &c, int &chunk, bool &packed) {
   const int lane = threadIdx.x & 63;
@@ -234,13 +266,13 @@ __device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedB
   while (last_lane(upto) <= unit && i0 + 64 < b.n_seqs) {  // (the unit is one of those counted)
     unit -= last_lane(upto);
     i0 += 64;
-    upto = lanes_up_to(units_in_lane(member_in_lane(L, b, i0 + lane, p.chunk), packed));
+    upto = lanes_up_to(units_in_lane(member_in_lane<RB>(L, b, i0 + lane, p.chunk), packed));
   }
   const unsigned long long behind = __ballot(upto > unit);
   const int k = uniform(behind ? __ffsll(behind) - 1 : 63);
   if (k > 0) unit -= __builtin_amdgcn_readlane(upto, k - 1);
   x.i = i0 + k < b.n_seqs ? i0 + k : b.n_seqs - 1;
-  const Member m = i0 ? member_in_lane(L, b, x.i, p.chunk) : members[k];  // (the same in every lane)
+  const Member m = i0 ? member_in_lane<RB>(L, b, x.i, p.chunk) : members[k];  // (the same in every lane)
   x.s = Sequence{uniform(m.s.row0), uniform(m.s.n_new), uniform(m.s.total), uniform(m.s.slot), true, false};
   x.s.slot_ok = x.s.slot >= 0 && x.s.slot < L.max_seqs;
   c = Chunks{uniform(m.c.n_kept), uniform(m.c.n_win), uniform(m.c.nq), uniform(m.c.rows), uniform(m.c.packed), uniform(m.c.chunk)};
@@ -249,10 +281,10 @@ __device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedB
   x.first = 0;
   if (blocks > 1) {
     chunk = unit / blocks;
-    x.first = 16 * (unit - chunk * blocks);
+    x.first = 16 * RB * (unit - chunk * blocks);
   }
   const int left = x.s.n_new * L.R - x.first;
-  x.count = left < 16 ? left : 16;
+  x.count = left < 16 * RB ? left : 16 * RB;
   return x;
 }
 
@@ -260,18 +292,16 @@ __device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedB
 template <int NG>
 struct State {
   float4_t o[8];      // packed: positions 16n + 4g + reg; full rows: channels 8 (4g + reg) + n
-  float4_t w[NG];     // packed: sum of the rounded weights that met the codes, in every register
-  float m, l, z[NG];  // reference; this lane's share of the sum of weights, of weights times zeros
+  float m, l, z[NG];  // reference; this lane's share of the sum of weights, of weights times zeros less the middle codes
+  float4_t by_matrix;  // (zeros_by_matrix) the sums of weights times zeros, group by group, in the lanes of g = 0
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int n = 0; n < 8; ++n) o[n] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     m = kNothing;
     l = 0.0f;
+    by_matrix = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      w[g] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-      z[g] = 0.0f;
-    }
+    for (int g = 0; g < NG; ++g) z[g] = 0.0f;
   }
   // Moves the references up where a lane holds a logarithm too far above its row's.
   __device__ __forceinline__ void refer(float top) {
@@ -282,24 +312,21 @@ struct State {
     m = to;
     l *= f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      z[g] *= f;
-      w[g] *= f;
-    }
+    for (int g = 0; g < NG; ++g) z[g] *= f;
+    if (zeros_by_matrix(NG)) by_matrix *= f;
 #pragma unroll
     for (int n = 0; n < 8; ++n) o[n] *= f;
   }
 };
 
-// One tile of packed rows.  MASKED: some of its rows are behind the chunk's end (what stands there may be anything) or
-// behind what some query sees.  left: rows of the tile before the end; seen: before the last one that the lane's row
-// sees.  alpha: on the scores, with the code's unit.
-template <int NG, int FMT, bool MASKED>
-__device__ __forceinline__ void take_tile(State<NG> &st, const Tile<NG, FMT> &t, const half8_t (&qb)[4], const float (&qs)[NG], float alpha,
-                                          int left, int seen, int g, int c) {
+// One tile of packed rows for RB blocks of query rows.  MASKED: some of its rows are behind the chunk's end (what stands
+// there may be anything) or behind what some query sees.  left: rows of the tile before the end; seen: before the last one
+// that the lane's row sees.  queries(r, j): block r's B operand for key dwords j; alpha: on the scores, with the code's unit.
+template <int NG, int FMT, int RB, bool MASKED, class Q, class Next>
+__device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t, const Next &next, const Q &queries, const float (&qs)[RB][NG],
+                                          const float (&alpha)[RB], int left, const int (&seen)[RB], int g, int c) {
   typedef PairSlot<NG> Slot;
-  // scale (of keys: times alpha) and zero (of values: with the middle code in it); the logarithm of the largest scale of
-  // the lane's row of values
+  // scale and zero (of values: with the middle code in it); the logarithm of the largest scale of the lane's row of values
   float scale[NG], zero[NG], most = 0.0f;
 #pragma unroll
   for (int q = 0; q < NG; ++q) {
@@ -307,60 +334,97 @@ __device__ __forceinline__ void take_tile(State<NG> &st, const Tile<NG, FMT> &t,
     const float2 pair = t.pairs[q].value();
     const bool there = !MASKED || 16 * slot.block + 4 * g + slot.token < left;
     const float x = there ? pair.x : 0.0f, z = there ? pair.y : 0.0f;
+    scale[q] = x;
     if (NG == 1) {  // (keys and values side by side)
-      scale[q] = x * (slot.values ? 1.0f : alpha);
       zero[q] = fmaf(x, slot.values ? kMidCode : 0.0f, z);
       most = slot.values ? x : 0.0f;
     } else if (q < NG / 2) {
-      scale[q] = x * alpha;
       zero[q] = z;
     } else {
-      scale[q] = x;
       zero[q] = fmaf(x, kMidCode, z);
       most = fmaxf(most, x);
     }
   }
-  most = row_max(most);
-  float s[8], top = -INFINITY;
+  next.pairs(t);
+  most = fmaxf(__builtin_amdgcn_logf(row_max(most)), kLowestLog);
+  // Broadcasts of a pair serve all blocks of rows; those of the next pairs wait (side by side they would fill the registers).
+  auto separate = [] {
+    if (RB > 1) __builtin_amdgcn_sched_barrier(0);
+  };
+  if (RB > 1) __atomic_signal_fence(__ATOMIC_ACQ_REL);  // (the queries are read again: holding them takes 32 registers)
+  float s[RB][8], top[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) top[b] = -INFINITY;
   const unsigned mask = 0x00f000f0u;
   unrolled<0, 2>([&](auto I) {
     constexpr int i = I();
-    float4_t acc[NG];
+    float4_t acc[RB][NG], x[RB];
 #pragma unroll
-    for (int n = 0; n < NG; ++n) acc[n] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b = 0; b < RB; ++b) {
+      x[b] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < NG; ++n) acc[b][n] = x[b];
+      if (zeros_by_matrix(NG)) x[b] = mfma(t.k_zero[i].value(), qs[b][0], x[b]);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const unsigned w = t.k[i][j];
-      acc[j * NG / 4] = mfma(as_half8((w << 4) & mask, w & mask, (w >> 4) & mask, (w >> 8) & mask), qb[j], acc[j * NG / 4]);
+      const half8_t codes = as_half8((w << 4) & mask, w & mask, (w >> 4) & mask, (w >> 8) & mask);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) acc[b][j * NG / 4] = mfma(codes, queries(b, j), acc[b][j * NG / 4]);
     }
+    separate();
     unrolled<0, 4>([&](auto R) {
       constexpr int r = R();
-      float x = 0.0f;
+      float codes[RB];
       unrolled<0, NG>([&](auto N) {
         constexpr int n = N(), q = Slot::load_of(0, i, r, n), lane = Slot::lane_of(0, i, r, n);
-        x = n == 0 ? of_lane<lane>(zero[q]) * qs[0] : fmaf(of_lane<lane>(zero[q]), qs[n], x);
-        x = fmaf(of_lane<lane>(scale[q]), acc[n][r], x);
+        const float by = of_lane<lane>(scale[q]), z = of_lane<lane>(zero[q]);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          if (!zeros_by_matrix(NG)) x[b][r] = n == 0 ? z * qs[b][0] : fmaf(z, qs[b][n], x[b][r]);
+          codes[b] = n == 0 ? by * acc[b][0][r] : fmaf(by, acc[b][n][r], codes[b]);
+        }
       });
-      const bool there = !MASKED || 16 * i + 4 * g + r < min(left, seen);
-      s[4 * i + r] = there ? x : -INFINITY;
-      top = fmaxf(top, s[4 * i + r]);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const bool there = !MASKED || 16 * i + 4 * g + r < min(left, seen[b]);
+        s[b][4 * i + r] = there ? fmaf(codes[b], alpha[b], x[b][r]) : -INFINITY;
+        top[b] = fmaxf(top[b], s[b][4 * i + r]);
+      }
+      separate();
     });
   });
-  st.refer(top + fmaxf(__builtin_amdgcn_logf(most), kLowestLog));
-  half8_t pb[NG];
+  next.keys(t);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) st[b].refer(top[b] + most);
+  half8_t pb[RB][NG];
   unrolled<0, 8>([&](auto I) {
     constexpr int i = I() / 4, r = I() % 4;
-    const float p = __builtin_amdgcn_exp2f(s[I()] - st.m);
-    st.l += p;
+    float p[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      p[b] = __builtin_amdgcn_exp2f(s[b][I()] - st[b].m);
+      st[b].l += p[b];
+    }
+    if (zeros_by_matrix(NG)) {
+      const float z = from_lane<Slot::lane_of(1, i, r, 0)>(zero[Slot::load_of(1, i, r, 0)]);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) st[b].by_matrix = mfma(z, p[b], st[b].by_matrix);
+    }
     unrolled<0, NG>([&](auto N) {
       constexpr int n = N(), q = Slot::load_of(1, i, r, n), lane = Slot::lane_of(1, i, r, n);
-      st.z[n] = fmaf(of_lane<lane>(zero[q]), p, st.z[n]);
-      pb[n][I()] = (_Float16)(of_lane<lane>(scale[q]) * p);
-    });
-  });
-  const half8_t one = as_half8(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
+      const float by = of_lane<lane>(scale[q]), z = of_lane<lane>(zero[q]);
 #pragma unroll
-  for (int n = 0; n < NG; ++n) st.w[n] = mfma(one, pb[n], st.w[n]);
+      for (int b = 0; b < RB; ++b) {
+        if (!zeros_by_matrix(NG)) st[b].z[n] = fmaf(z, p[b], st[b].z[n]);
+        pb[b][n][I()] = (_Float16)(by * p[b]);
+        const half2_t middle = {-(_Float16)kMidCode, -(_Float16)kMidCode};
+        if (r % 2) st[b].z[n] = __builtin_amdgcn_fdot2(half2_t{pb[b][n][I() & ~1], pb[b][n][I()]}, middle, st[b].z[n], false);
+      }
+    });
+    separate();
+  });
 #pragma unroll
   for (int n = 0; n < 8; ++n) {
     unsigned a[4];
@@ -369,20 +433,30 @@ __device__ __forceinline__ void take_tile(State<NG> &st, const Tile<NG, FMT> &t,
       const unsigned w = t.v[i / 2][2 * (i % 2) + n / 4];
       a[i] = (n % 4 == 0 ? w << 4 : n % 4 == 1 ? w : n % 4 == 2 ? w >> 4 : w >> 8) & mask;
     }
-    st.o[n] = mfma(as_half8(a[0], a[1], a[2], a[3]), pb[n * NG / 8], st.o[n]);
+    const half8_t codes = as_half8(a[0], a[1], a[2], a[3]);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) st[b].o[n] = mfma(codes, pb[b][n * NG / 8], st[b].o[n]);
   }
+  next.values(t);
 }
 
-template <class T>
+template <class T, int RB>
 struct Lds {
   union alignas(16) {
-    T q[16][kD + 8];  // the queries; for packed rows a head's channels in the order of the key codes
+    T q[16 * RB][kD + 8];         // the queries ...
+    _Float16 h[16 * RB][kD + 8];  // ... for packed rows: as fp16 numbers, a head's channels in the order of the key codes
     float acc[kWaves][16][kRowStride];
   };
   float m[kWaves][16], l[kWaves][16];
+  float unit[16 * RB];  // what 1 stands for in h
   int bad;
   Member members[64];
 };
+
+// The last token that a row of the unit sees (rows past the last one: as that).
+__device__ __forceinline__ int last_token(const PagedLayout &L, const RowBlock &x, int row) {
+  return x.s.total - x.s.n_new + quotient(x.first + (row < x.count ? row : x.count - 1), L.recip_R);
+}
 
 // Pages of the wavefront's tiles k0 .. k0 + 31 of a chunk [begin, end) of packed rows, two blocks of 16 tokens each: lane
 // 2k + i holds tile k0 + k's block i.
@@ -402,14 +476,15 @@ __device__ __forceinline__ int pages_of_tiles(const PagedLayout &L, const PagedB
 }
 
 // The wavefront's share of a chunk of packed rows.  ids: pages_of_tiles of its first tiles.
-template <class T, int NG, int FMT>
-__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T> &lds, const RowBlock &x, const Chunks &ch,
-                                            int chunk, int h, int ids, State<NG> &st, bool &bad) {
+template <class T, int NG, int FMT, int RB>
+__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T, RB> &lds, const RowBlock &x, const Chunks &ch,
+                                            int chunk, int h, int ids, State<NG> (&st)[RB], bool &bad) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int last = x.s.total - x.s.n_new + (x.first + (c < x.count ? c : x.count - 1)) / L.R;  // lane's row: the last token it sees
-  const int seen = last + 1 - L.S;  // packed rows that the lane's row sees; all of them see the first row's
+  int seen[RB];  // packed rows that the lane's row sees; all rows see the first one's
+#pragma unroll
+  for (int r = 0; r < RB; ++r) seen[r] = last_token(L, x, 16 * r + c) + 1 - L.S;
   const int begin = chunk * ch.chunk, end = min(ch.nq, begin + ch.chunk);
-  const int all_see = min(end, x.s.total - x.s.n_new + x.first / L.R + 1 - L.S);
+  const int all_see = min(end, last_token(L, x, 0) + 1 - L.S);
   const int n_tiles = (end - begin + kTile - 1) / kTile, mine = n_tiles > wave ? (n_tiles - wave + kWaves - 1) / kWaves : 0;
   const uint8_t *head_part = L.pages + (long long)h * L.part_bytes;
   const long long page_stride = (long long)L.Hk * L.part_bytes;
@@ -423,102 +498,110 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
     pair_lane[q] = (slot.values ? L.vm_at : L.km_at) + kPair * ((4 * g + slot.token) * NG + slot.group);
     pair_block[q] = slot.block;
   }
-  // The wavefront's k-th tile, of those that `ids` holds from the k0-th on (blocks past the end: of page 0).
-  // Codes are read once per row block, by instructions that take whole lines: streaming loads.
-  auto load = [&](Tile<NG, FMT> &t, int k, int k0) {
+  // Loads of the wavefront's k-th tile, of those that `ids` holds from the k0-th on (blocks past the end: of page 0).
+  // Codes are read once per unit, by instructions that take whole lines: streaming loads.
+  struct Next {
+    const PagedLayout &L;
+    const unsigned k_lane, v_lane, (&pair_lane)[NG];
+    const bool (&pair_block)[NG];
+    const unsigned zero_lane;
     const uint8_t *part[2];
     unsigned place[2];
+    __device__ __forceinline__ uint4_t codes(int i, unsigned lane) const {
+      return __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(part[i] + place[i] * (kD / 2) + lane));
+    }
+    __device__ __forceinline__ void pairs(Tile<NG, FMT> &t) const {
+      const uint8_t *p0 = part[0] + place[0] * (NG * kPair), *p1 = part[1] + place[1] * (NG * kPair);
+#pragma unroll
+      for (int q = 0; q < NG; ++q) t.pairs[q].load((pair_block[q] ? p1 : p0) + pair_lane[q]);
+    }
+    __device__ __forceinline__ void keys(Tile<NG, FMT> &t) const {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        t.k[i] = codes(i, k_lane);
+        if (zeros_by_matrix(NG)) t.k_zero[i].load(part[i] + place[i] * (NG * kPair) + zero_lane);
+      }
+    }
+    __device__ __forceinline__ void values(Tile<NG, FMT> &t) const {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) t.v[i] = codes(i, v_lane);
+    }
+  };
+  auto tile = [&](int k, int k0) {
+    Next x{L, k_lane, v_lane, pair_lane, pair_block, L.km_at + (c * NG + g) * kPair, {}, {}};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int id = __builtin_amdgcn_readlane(ids, 2 * (k - k0) + i);
       const int te = begin + kTile * (wave + kWaves * k) + 16 * i;
-      place[i] = te & ((1 << L.page_log2) - 1);
-      part[i] = head_part + id * page_stride;
-      const uint8_t *codes = part[i] + place[i] * (kD / 2);
-      t.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(codes + k_lane));
-      t.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(codes + v_lane));
+      x.place[i] = te & ((1 << L.page_log2) - 1);
+      x.part[i] = head_part + id * page_stride;
     }
-#pragma unroll
-    for (int q = 0; q < NG; ++q) {
-      const uint8_t *p0 = part[0] + place[0] * (NG * kPair), *p1 = part[1] + place[1] * (NG * kPair);
-      t.pairs[q].load((pair_block[q] ? p1 : p0) + pair_lane[q]);
-    }
+    return x;
   };
-  Tile<NG, FMT> even, odd;
-  if (mine > 0) load(even, 0, 0);
-  // B operand: row c's queries at the reordered positions of key dword 4g + j, as fp16 numbers.  bf16 queries are
-  // brought to fp16's range by one power of two: what that makes subnormal is 2^-25 of the largest.
-  half8_t qb[4];
-  float qs[NG], scale = L.sm_scale * kLog2e, alpha = scale * kCodeUnit;
-  {
-    typedef T t8 __attribute__((ext_vector_type(8)));
-    t8 v[4];
+  Tile<NG, FMT> t;
+  if (mine > 0) {
+    const Next x = tile(0, 0);
+    x.pairs(t);
+    x.keys(t);
+    x.values(t);
+  }
+  // B operand of block r: row c's queries at the reordered positions of key dword 4g + j.  One block's stay in registers,
+  // more are read for every tile.
+  half8_t held[RB == 1 ? 4 : 1];
+  auto queries = [&](int r, int j) { return RB == 1 ? held[j] : *reinterpret_cast<const half8_t *>(&lds.h[16 * r + c][8 * (4 * g + j)]); };
+  float qs[RB][NG], alpha[RB];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const t8 *>(&lds.q[c][8 * (4 * g + j)]);
+  for (int r = 0; r < RB; ++r) {
+    const float scale = L.sm_scale * kLog2e * lds.unit[16 * r + c];
+    alpha[r] = scale * kCodeUnit;
 #pragma unroll
-    for (int n = 0; n < NG; ++n) qs[n] = 0.0f;
-    float to_half = 1.0f;
-    if constexpr (!__is_same(T, _Float16)) {
-      float most = 0.0f;
+    for (int n = 0; n < NG; ++n) qs[r][n] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+      const half8_t v = *reinterpret_cast<const half8_t *>(&lds.h[16 * r + c][8 * (4 * g + j)]);
+      if (RB == 1) held[j] = v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)v[j][e]));
-      most = row_max(most);
-      most = fmaxf(most, __shfl_xor(most, 16));
-      most = fmaxf(most, __shfl_xor(most, 32));
-      const int exponent = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;  // most in [2^(e-1), 2^e)
-      to_half = __builtin_amdgcn_ldexpf(1.0f, 14 - exponent < 126 ? 14 - exponent : 126);
-      alpha /= to_half;
+      for (int e = 0; e < 8; ++e) qs[r][j * NG / 4] += (float)v[e];
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        qs[j * NG / 4] += (float)v[j][e];
-        if constexpr (__is_same(T, _Float16))
-          qb[j][e] = v[j][e];
-        else
-          qb[j][e] = (_Float16)((float)v[j][e] * to_half);
-      }
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
-      qs[n] += __shfl_xor(qs[n], 16);
-      qs[n] += __shfl_xor(qs[n], 32);
-      qs[n] *= scale;
+      qs[r][n] += __shfl_xor(qs[r][n], 16);
+      qs[r][n] += __shfl_xor(qs[r][n], 32);
+      qs[r][n] *= scale;
+    }
+    if (zeros_by_matrix(NG)) {  // (the matrix product's B operand: a group per row of lanes)
+#pragma unroll
+      for (int n = 1; n < NG; ++n) qs[r][0] = g == n ? qs[r][n] : qs[r][0];
     }
   }
-  // Whole tiles that every query sees, two buffers in turn; then the others (at the chunk's end).  The lanes hold the pages
-  // of 32 tiles, and the next tile is on its way while one is worked on (the last one's loads are repeated: no branch
-  // between loads and what they hide behind): 30 tiles a turn.
+  // Whole tiles that every query sees, then the others (at the chunk's end).  The lanes hold the pages of 32 tiles, and the
+  // next tile's pairs, key codes and value codes are asked for as soon as this one's have been used (the last one's loads are
+  // repeated: no branch between loads and what they hide behind): 31 tiles a turn.
   const int whole_tiles = all_see > begin ? (all_see - begin) / kTile : 0;
   const int whole = whole_tiles > wave ? (whole_tiles - wave + kWaves - 1) / kWaves : 0;
-  for (int k0 = 0; k0 < mine; k0 += 30) {
+  for (int k0 = 0; k0 < mine; k0 += 31) {
     if (k0 > 0) ids = pages_of_tiles(L, b, x.i, begin, end, k0, bad);
-    const int stop = min(mine, k0 + 30);
+    const int stop = min(mine, k0 + 31), stop_whole = min(stop, whole);
     int k = k0;
-    for (const int stop_whole = min(stop, whole); k + 1 < stop_whole; k += 2) {
-      load(odd, k + 1, k0);
-      take_tile<NG, FMT, false>(st, even, qb, qs, alpha, 0, 0, g, c);
-      load(even, min(k + 2, mine - 1), k0);
-      take_tile<NG, FMT, false>(st, odd, qb, qs, alpha, 0, 0, g, c);
-    }
+    for (; k < stop_whole; ++k)
+      take_tile<NG, FMT, RB, false>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, 0, seen, g, c);
     for (; k < stop; ++k) {
       const int te0 = begin + kTile * (wave + kWaves * k);
-      load(odd, min(k + 1, mine - 1), k0);
-      take_tile<NG, FMT, true>(st, even, qb, qs, alpha, end - te0, seen - te0, g, c);
-      even = odd;
+      int seen_here[RB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) seen_here[r] = seen[r] - te0;
+      take_tile<NG, FMT, RB, true>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, end - te0, seen_here, g, c);
     }
   }
 }
 
 // ... of a chunk of full-precision rows: the u-th of the kept and the ring tokens, in the order of their numbers.
-template <class T, int NG>
-__device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T> &lds, const RowBlock &x, const Chunks &ch, int chunk, int h,
-                                          State<NG> &st) {
+template <class T, int NG, int RB>
+__device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T, RB> &lds, const RowBlock &x, const Chunks &ch, int chunk, int h,
+                                          int block, State<NG> &st) {
   typedef T t8 __attribute__((ext_vector_type(8)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int last = x.s.total - x.s.n_new + (x.first + (c < x.count ? c : x.count - 1)) / L.R;
+  const int last = last_token(L, x, 16 * block + c);
   const float scale = L.sm_scale * kLog2e;
   const int n_full = ch.n_kept + ch.n_win, begin = chunk * kPagedRowsPerChunk, end = min(n_full, begin + kPagedRowsPerChunk);
   const long long head = ((long long)x.s.slot * L.Hk + h) * (L.W + L.S) * kD;
@@ -532,7 +615,7 @@ __device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T> &ld
   auto token_of = [&](int u) { return u < ch.n_kept ? u : first_recent + u - ch.n_kept; };
   t8 qb[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) qb[j] = *reinterpret_cast<const t8 *>(&lds.q[c][32 * j + 8 * g]);
+  for (int j = 0; j < 4; ++j) qb[j] = *reinterpret_cast<const t8 *>(&lds.q[16 * block + c][32 * j + 8 * g]);
   for (int u0 = begin + kTile * wave; u0 < end; u0 += kTile * kWaves) {
     t8 kb[2][4], vb[2][4];
 #pragma unroll
@@ -579,27 +662,31 @@ __device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T> &ld
   }
 }
 
-template <class T, int NG, int FMT>
-__global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attention_kernel(const PagedLayout L, const PagedBatch b, const TokenRows q,
-                                                                                    const Out out, int n_row_chunks) {
+template <class T, int NG, int FMT, int RB>
+__global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_attention_kernel(const PagedLayout L, const PagedBatch b,
+                                                                                        const TokenRows q, const Out out, int n_row_chunks) {
   typedef Piece<T, 8> P;
-  __shared__ Lds<T> lds;
+  __shared__ Lds<T, RB> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int h = blockIdx.x;  // (heads side by side: a head's units, row blocks of one chunk among them, share a chiplet's L2)
   const unsigned long long places = *reinterpret_cast<const unsigned long long *>(L.k_place + h * kD + 8 * c);
   const int p = threadIdx.x % kD, packed_channel = L.v_offset[h * kD + 8 * (p & 15) + (p >> 4)] / 2;  // of the output place it writes
-  const BatchPlan plan = plan_batch(L, b, gridDim.y, lds.members);
+  const BatchPlan plan = plan_batch<RB>(L, b, gridDim.y, lds.members);
   __syncthreads();
   for (int unit = blockIdx.y; unit < plan.units; unit += gridDim.y) {
     int chunk;
     bool packed;
     Chunks ch;
-    const RowBlock x = find_unit(L, b, plan, lds.members, unit, ch, chunk, packed);
+    const RowBlock x = find_unit<RB>(L, b, plan, lds.members, unit, ch, chunk, packed);
     // the queries, sixteen threads a row, rows past the last one repeat it; the first pages meanwhile
     static_assert(64 * kWaves == 16 * 16, "one piece of a row per thread");
     const int query = threadIdx.x >> 4;
-    const QueryRow from = query_row(L, x, h, query < x.count ? query : x.count - 1);
-    const P mine = *reinterpret_cast<const P *>((const T *)q.p + from.token * q.stride + from.head * kD + 8 * c);
+    P mine[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const QueryRow from = query_row(L, x, h, min(16 * r + query, x.count - 1));
+      mine[r] = *reinterpret_cast<const P *>((const T *)q.p + from.token * q.stride + from.head * kD + 8 * c);
+    }
     bool bad = false;
     int ids = 0;
     if (packed) {
@@ -611,80 +698,108 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG)) void paged_attentio
       lds.bad = !x.s.slot_ok;
       if (!x.s.slot_ok) atomicOr(L.errors, SKVQ_PAGED_BAD_SLOT);
     }
-    if (packed) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) lds.q[query][(places >> (8 * e)) & 0xffu] = mine[e];
-    } else {
-      *reinterpret_cast<P *>(&lds.q[query][8 * c]) = mine;
+    for (int r = 0; r < RB; ++r) {
+      if (packed) {
+        // bf16 queries are brought to fp16's range by one power of two: what that makes subnormal is 2^-25 of the largest.
+        float to_half = 1.0f;
+        if constexpr (!__is_same(T, _Float16)) {
+          float largest = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf((float)mine[r][e]));
+          largest = row_max(largest);
+          const int exponent = largest > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(largest) : 0;  // largest in [2^(e-1), 2^e)
+          to_half = __builtin_amdgcn_ldexpf(1.0f, exponent < 126 ? exponent : 126);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          _Float16 &to = lds.h[16 * r + query][(places >> (8 * e)) & 0xffu];
+          if constexpr (__is_same(T, _Float16))
+            to = mine[r][e];
+          else
+            to = (_Float16)((float)mine[r][e] * to_half);
+        }
+        if (c == 0) lds.unit[16 * r + query] = 1.0f / to_half;
+      } else {
+        *reinterpret_cast<P *>(&lds.q[16 * r + query][8 * c]) = mine[r];
+      }
     }
     __syncthreads();
-    State<NG> st;
-    st.clear();
-    if (packed)
-      take_packed<T, NG, FMT>(L, b, lds, x, ch, chunk, h, ids, st, bad);
-    else if (x.s.slot_ok)
-      take_rows<T, NG>(L, lds, x, ch, chunk, h, st);
+    State<NG> st[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) st[r].clear();
+    if (packed) {
+      take_packed<T, NG, FMT, RB>(L, b, lds, x, ch, chunk, h, ids, st, bad);
+    } else if (x.s.slot_ok) {
+#pragma unroll
+      for (int r = 0; r < RB; ++r) take_rows<T, NG, RB>(L, lds, x, ch, chunk, h, r, st[r]);
+    }
 
     // The wavefronts' states: sums over the lanes of a row, then one reference for the workgroup.
-    st.l += __shfl_xor(st.l, 16);
-    st.l += __shfl_xor(st.l, 32);
-#pragma unroll
-    for (int n = 0; n < NG; ++n) {
-      st.z[n] += __shfl_xor(st.z[n], 16);
-      st.z[n] += __shfl_xor(st.z[n], 32);
-      st.z[n] -= kMidCode * st.w[n][0];
-    }
-    if (g == 0) {
-      lds.m[wave][c] = st.m;
-      lds.l[wave][c] = st.l;
-    }
-    __syncthreads();  // (also: the queries in LDS are no longer needed)
-    if (bad) {
-      lds.bad = 1;
-      atomicOr(L.errors, SKVQ_PAGED_BAD_PAGE);
-    }
-    float top = lds.m[0][c];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds.m[w][c]);
-    const float f = __builtin_amdgcn_exp2f(st.m - top);
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      float4_t y = st.o[n];
-      if (packed) {
-        y = (y * kCodeUnit + st.z[n * NG / 8]) * f;
-        *reinterpret_cast<float4_t *>(&lds.acc[wave][c][16 * n + 4 * g]) = y;
-      } else {
-        y *= f;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) lds.acc[wave][c][8 * (4 * g + r) + n] = y[r];
-      }
-    }
-    __syncthreads();
     const int n_partials = ch.rows + ch.packed, most = kPagedMaxSplits + n_row_chunks;
     const int channel = packed ? packed_channel : p;
-    for (int row = threadIdx.x / kD; row < x.count; row += 64 * kWaves / kD) {
-      float acc = lds.acc[0][row][p], m = lds.m[0][row], l = 0.0f;
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        acc += lds.acc[w][row][p];
-        m = fmaxf(m, lds.m[w][row]);
+    for (int r = 0; r < RB; ++r) {
+      State<NG> &own = st[r];
+      own.l += __shfl_xor(own.l, 16);
+      own.l += __shfl_xor(own.l, 32);
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        own.z[n] += __shfl_xor(own.z[n], 16);
+        own.z[n] += __shfl_xor(own.z[n], 32);
+        if (zeros_by_matrix(NG)) own.z[n] += __shfl(own.by_matrix[n], c);
       }
+      if (r > 0) __syncthreads();  // (the block before has been read out of LDS)
+      if (g == 0) {
+        lds.m[wave][c] = own.m;
+        lds.l[wave][c] = own.l;
+      }
+      __syncthreads();  // (also: the queries in LDS are no longer needed)
+      if (r == 0 && bad) {
+        lds.bad = 1;
+        atomicOr(L.errors, SKVQ_PAGED_BAD_PAGE);
+      }
+      float top = lds.m[0][c];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) l += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - m);
-      if (lds.bad) l = NAN;
-      const QueryRow qr = query_row(L, x, h, row);
-      float *to = L.workspace + ((long long)qr.token * L.Hq + qr.head) * most * kPartialStride;
-      if (n_partials == 1) {
-        store_out<T>(L, out, qr, channel, acc / l);
-      } else {
-        float *part = to + (packed ? ch.rows + chunk : chunk) * kPartialStride;
-        part[4 + channel] = acc;
-        if (p == 0) {
-          part[0] = m;
-          part[1] = l;
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds.m[w][c]);
+      const float f = __builtin_amdgcn_exp2f(own.m - top);
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        float4_t y = own.o[n];
+        if (packed) {
+          y = (y * kCodeUnit + own.z[n * NG / 8]) * f;
+          *reinterpret_cast<float4_t *>(&lds.acc[wave][c][16 * n + 4 * g]) = y;
+        } else {
+          y *= f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) lds.acc[wave][c][8 * (4 * g + k) + n] = y[k];
         }
       }
-      if (p == 0 && !packed && chunk == 0) to[2] = __uint_as_float((unsigned)n_partials);  // (for the merge)
+      __syncthreads();
+      for (int row = threadIdx.x / kD; row < min(x.count - 16 * r, 16); row += 64 * kWaves / kD) {
+        float acc = lds.acc[0][row][p], m = lds.m[0][row], l = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+          acc += lds.acc[w][row][p];
+          m = fmaxf(m, lds.m[w][row]);
+        }
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) l += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - m);
+        if (lds.bad) l = NAN;
+        const QueryRow qr = query_row(L, x, h, 16 * r + row);
+        float *to = L.workspace + ((long long)qr.token * L.Hq + qr.head) * most * kPartialStride;
+        if (n_partials == 1) {
+          store_out<T>(L, out, qr, channel, acc / l);
+        } else {
+          float *part = to + (packed ? ch.rows + chunk : chunk) * kPartialStride;
+          part[4 + channel] = acc;
+          if (p == 0) {
+            part[0] = m;
+            part[1] = l;
+          }
+        }
+        if (p == 0 && !packed && chunk == 0) to[2] = __uint_as_float((unsigned)n_partials);  // (for the merge)
+      }
     }
   }
 }
@@ -748,22 +863,22 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
   }
 }
 
-template <class T, int NG>
+template <class T, int NG, int RB>
 void launch_chunks(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
   const dim3 grid(L.Hk, groups), threads(64 * kWaves);
   switch (L.meta_fmt) {
-    case SKVQ_META_F32: paged_attention_kernel<T, NG, SKVQ_META_F32><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
-    case SKVQ_META_F16: paged_attention_kernel<T, NG, SKVQ_META_F16><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
-    default: paged_attention_kernel<T, NG, SKVQ_META_FP8_E4M3><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    case SKVQ_META_F32: paged_attention_kernel<T, NG, SKVQ_META_F32, RB><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    case SKVQ_META_F16: paged_attention_kernel<T, NG, SKVQ_META_F16, RB><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
+    default: paged_attention_kernel<T, NG, SKVQ_META_FP8_E4M3, RB><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
   }
 }
 
-template <class T>
+template <class T, int RB>
 hipError_t launch_typed(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
   switch (L.NG) {
-    case 1: launch_chunks<T, 1>(L, b, q, out, row_chunks, groups, s); break;
-    case 2: launch_chunks<T, 2>(L, b, q, out, row_chunks, groups, s); break;
-    default: launch_chunks<T, 4>(L, b, q, out, row_chunks, groups, s); break;
+    case 1: launch_chunks<T, 1, RB>(L, b, q, out, row_chunks, groups, s); break;
+    case 2: launch_chunks<T, 2, RB>(L, b, q, out, row_chunks, groups, s); break;
+    default: launch_chunks<T, 4, RB>(L, b, q, out, row_chunks, groups, s); break;
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -778,16 +893,20 @@ hipError_t launch_paged_attention(const PagedLayout &L, const skvq_batch &batch,
   const PagedBatch b = batch_of(batch);
   const int row_chunks = paged_row_chunks(L.W, L.S);
   // Lengths are not known here: as many workgroups as the chip holds at once, over the kv heads, unless there can be no
-  // more units than that (every query token of a sequence of its own, as long as the page table allows).
-  const long long rows = (long long)b.n_tokens * L.R, blocks = rows / 16 + (b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens);
+  // more units than that (every query token of a sequence of its own, as long as the page table allows).  Where a sequence
+  // has more than 16 rows per kv head on average, a unit holds two blocks of them.
+  const long long rows = (long long)b.n_tokens * L.R;
+  const int row_blocks = rows > 16LL * b.n_seqs ? 2 : 1;
+  const long long blocks = rows / (16 * row_blocks) + (b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens);
   long long splits = ((long long)b.table_stride << L.page_log2) / kPagedMinChunk + 1;
   if (splits > kPagedMaxSplits) splits = kPagedMaxSplits;
-  const long long units = blocks * (row_chunks + splits), most = (long long)groups_per_cu(L.NG) * n_cus / L.Hk;
+  const long long units = blocks * (row_chunks + splits), most = (long long)groups_per_cu(L.NG, row_blocks) * n_cus / L.Hk;
   if (units > 1 << 30) return hipErrorInvalidValue;  // (counted in 32 bits)
   const unsigned groups = (unsigned)(units < most ? units : most > 0 ? most : 1);
   const Out o{out, out_stride, out_f32};
-  return L.dtype == SKVQ_DTYPE_BF16 ? launch_typed<__bf16>(L, b, q, o, row_chunks, groups, s)
-                                    : launch_typed<_Float16>(L, b, q, o, row_chunks, groups, s);
+  if (L.dtype == SKVQ_DTYPE_BF16)
+    return row_blocks == 2 ? launch_typed<__bf16, 2>(L, b, q, o, row_chunks, groups, s) : launch_typed<__bf16, 1>(L, b, q, o, row_chunks, groups, s);
+  return row_blocks == 2 ? launch_typed<_Float16, 2>(L, b, q, o, row_chunks, groups, s) : launch_typed<_Float16, 1>(L, b, q, o, row_chunks, groups, s);
 }
 
 }  // namespace skvq

@@ -140,6 +140,21 @@ def test_heads_and_query_tokens(B, hq, hk, new):
     b.check_attention([0, 1], [new, min(new, 2)])
 
 
+@pytest.mark.parametrize("group,meta,dtype", FORMATS)
+def test_many_rows_of_all_sizes(B, group, meta, dtype):
+    """More than 16 query rows per kv head on average, some sequences with fewer, none a multiple of 32; queries whose
+    rows differ by powers of two up to 2^20 (bf16) or 2^8 (fp16)."""
+    b = Both(B, hq=14, hk=2, group=group, meta=meta, dtype=dtype, sinks=2, page=32, n_pages=128, seed=29, max_tokens=800)
+    seqs, held = [2, 0, 3, 1], [400, 37, 700, 5]
+    b.append(seqs, held)
+    new = [9, 1, 5, 2]
+    size = 2.0 ** np.arange(-12, 9 if dtype is torch.bfloat16 else -3)
+    draw = b.draw
+    b.draw = lambda n, heads: draw(n, heads, b.rng.choice(size, (n, heads, 1)))
+    b.check_attention(seqs, new)
+    b.check_attention(seqs[1:], [5, 5, 5])
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("total", [16 + 15, 16 + 16, 16 + 17, 16 + 255, 16 + 256, 16 + 257, 16 + 600])
 def test_pages_and_tiles_end_anywhere(B, page, total):
