@@ -20,11 +20,12 @@
 // eight sequences of up to 40k tokens with two to eight new ones, four fp32 groups, from 119 to 115 us.
 //
 // The weight that multiplies a code is weight * scale: the reference counts log2 of the largest scale at hand in, so
-// that this product, rounded to fp16 (half a step of 2^-10; a second part as in the fixed cache's kernel would refine
-// what 16-bit outputs do not show), stays within fp16's normal numbers near the largest contributions.  The middle code
-// goes into the zero and the rounded weights' own sum (one more matrix instruction, against ones) is taken off as often:
-// only a code's distance from the middle feels the rounding (error of a flat average of 32k tokens against 64 bits,
-// beside the output's own rounding: 1.8e-4 -> 0.9e-4).  Zeros enter by fp32 sums: out = sum (w scale) code + sum w zero.
+// that this product stays within fp16's normal numbers near the largest contributions.  For fp16 outputs it is taken in
+// two parts, rounded (half a step of 2^-10) and the rest: one alone is an error as large as the output's own rounding
+// (16 sequences of 32k tokens, rms against 64 bits: 2.1e-4 with both, as of the rounding alone, 2.6e-4 with one; 2 to 3%
+// of the time).  bf16 outputs, of 8 bits, make do with one (1.7e-3 either way); there the middle code goes into the zero
+// and the rounded weights' own sum is taken off as often, so that only a code's distance from the middle feels the
+// rounding.  Zeros enter by fp32 sums: out = sum (w scale) code + sum w zero.
 //
 // Lengths are device data: every workgroup sums up the batch, finds the chunk size that fills the chip's workgroups
 // evenly (chunk_for) and its own units.  Bound by HBM for long contexts: 136 bytes per (token, kv head) at one group.
@@ -125,6 +126,10 @@ struct ZeroWord {  // a pair's zero
       return (float)w;
   }
 };
+
+// Whether a weight that meets codes has two parts.
+template <class T>
+constexpr bool two_parts() { return __is_same(T, _Float16); }
 
 // Zeros enter scores and outputs by products with the queries' sums and with the weights.  Of four groups, these are fp32
 // matrix instructions: 4 multiplications a lane and score, each with a broadcast before it, would be a quarter of the work.
@@ -322,11 +327,11 @@ struct State {
 // One tile of packed rows for RB blocks of query rows.  MASKED: some of its rows are behind the chunk's end (what stands
 // there may be anything) or behind what some query sees.  left: rows of the tile before the end; seen: before the last one
 // that the lane's row sees.  queries(r, j): block r's B operand for key dwords j; alpha: on the scores, with the code's unit.
-template <int NG, int FMT, int RB, bool MASKED, class Q, class Next>
+template <class T, int NG, int FMT, int RB, bool MASKED, class Q, class Next>
 __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t, const Next &next, const Q &queries, const float (&qs)[RB][NG],
                                           const float (&alpha)[RB], int left, const int (&seen)[RB], int g, int c) {
   typedef PairSlot<NG> Slot;
-  // scale and zero (of values: with the middle code in it); the logarithm of the largest scale of the lane's row of values
+  // scale and zero (of values: with the middle code in it, see above); the logarithm of the largest scale of the lane's row of values
   float scale[NG], zero[NG], most = 0.0f;
 #pragma unroll
   for (int q = 0; q < NG; ++q) {
@@ -336,12 +341,12 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
     const float x = there ? pair.x : 0.0f, z = there ? pair.y : 0.0f;
     scale[q] = x;
     if (NG == 1) {  // (keys and values side by side)
-      zero[q] = fmaf(x, slot.values ? kMidCode : 0.0f, z);
+      zero[q] = two_parts<T>() ? z : fmaf(x, slot.values ? kMidCode : 0.0f, z);
       most = slot.values ? x : 0.0f;
     } else if (q < NG / 2) {
       zero[q] = z;
     } else {
-      zero[q] = fmaf(x, kMidCode, z);
+      zero[q] = two_parts<T>() ? z : fmaf(x, kMidCode, z);
       most = fmaxf(most, x);
     }
   }
@@ -398,7 +403,7 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
   next.keys(t);
 #pragma unroll
   for (int b = 0; b < RB; ++b) st[b].refer(top[b] + most);
-  half8_t pb[RB][NG];
+  half8_t pb[RB][NG], rest[RB][NG];
   unrolled<0, 8>([&](auto I) {
     constexpr int i = I() / 4, r = I() % 4;
     float p[RB];
@@ -418,9 +423,13 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         if (!zeros_by_matrix(NG)) st[b].z[n] = fmaf(z, p[b], st[b].z[n]);
-        pb[b][n][I()] = (_Float16)(by * p[b]);
+        const float w = by * p[b];
+        pb[b][n][I()] = (_Float16)w;
         const half2_t middle = {-(_Float16)kMidCode, -(_Float16)kMidCode};
-        if (r % 2) st[b].z[n] = __builtin_amdgcn_fdot2(half2_t{pb[b][n][I() & ~1], pb[b][n][I()]}, middle, st[b].z[n], false);
+        if (two_parts<T>())
+          rest[b][n][I()] = (_Float16)(w - (float)pb[b][n][I()]);
+        else if (r % 2)
+          st[b].z[n] = __builtin_amdgcn_fdot2(half2_t{pb[b][n][I() & ~1], pb[b][n][I()]}, middle, st[b].z[n], false);
       }
     });
     separate();
@@ -435,7 +444,10 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
     }
     const half8_t codes = as_half8(a[0], a[1], a[2], a[3]);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) st[b].o[n] = mfma(codes, pb[b][n * NG / 8], st[b].o[n]);
+    for (int b = 0; b < RB; ++b) {
+      st[b].o[n] = mfma(codes, pb[b][n * NG / 8], st[b].o[n]);
+      if (two_parts<T>()) st[b].o[n] = mfma(codes, rest[b][n * NG / 8], st[b].o[n]);
+    }
   }
   next.values(t);
 }
@@ -584,13 +596,13 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
     const int stop = min(mine, k0 + 31), stop_whole = min(stop, whole);
     int k = k0;
     for (; k < stop_whole; ++k)
-      take_tile<NG, FMT, RB, false>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, 0, seen, g, c);
+      take_tile<T, NG, FMT, RB, false>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, 0, seen, g, c);
     for (; k < stop; ++k) {
       const int te0 = begin + kTile * (wave + kWaves * k);
       int seen_here[RB];
 #pragma unroll
       for (int r = 0; r < RB; ++r) seen_here[r] = seen[r] - te0;
-      take_tile<NG, FMT, RB, true>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, end - te0, seen_here, g, c);
+      take_tile<T, NG, FMT, RB, true>(st, t, tile(min(k + 1, mine - 1), k0), queries, qs, alpha, end - te0, seen_here, g, c);
     }
   }
 }
@@ -657,7 +669,7 @@ __device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T, RB>
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = vb[i / 4][i % 4][n];
       st.o[n] = mfma(a, hi, st.o[n]);
-      if constexpr (!__is_same(T, _Float16)) st.o[n] = mfma(a, lo, st.o[n]);  // (fp16 holds 11 bits of a weight, bf16 8)
+      st.o[n] = mfma(a, lo, st.o[n]);
     }
   }
 }
