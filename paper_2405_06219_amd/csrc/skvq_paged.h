@@ -111,6 +111,8 @@ hipError_t launch_paged_append(const PagedLayout &L, const RopeTable &tab, const
 hipError_t launch_paged_read(const PagedLayout &L, const skvq_batch &b, void *k, long long k_stride, void *v,
                              long long v_stride, int n_cus, hipStream_t s);
 
+// The most work (see plan) that a call can have.
+long long paged_most_work(const PagedLayout &L, const skvq_batch &b);
 hipError_t launch_paged_attention(const PagedLayout &L, const skvq_batch &b, TokenRows q, void *out, long long out_stride,
                                   float *out_f32, int n_cus, hipStream_t s);
 

@@ -333,7 +333,8 @@ int skvq_paged_attention(skvq_paged *c, const skvq_batch *batch, const void *q, 
   if (rc != SKVQ_OK) return rc;
   if (batch->n_tokens > c->max_tokens) return SKVQ_ERR_INVALID_ARG;
   if (empty) return SKVQ_OK;
-  if ((long long)batch->n_tokens * c->L.R >= 1 << 27) return SKVQ_ERR_UNSUPPORTED;  // (query rows: see quotient)
+  // (query rows: see quotient; work: counted in 32 bits)
+  if ((long long)batch->n_tokens * c->L.R >= 1 << 27 || paged_most_work(c->L, *batch) >= kPagedMostWork) return SKVQ_ERR_UNSUPPORTED;
   if (!rows_ok(q, q_stride, c->L.Hq) || (!out && !out_f32) || (out && !rows_ok(out, out_stride, c->L.Hq)) || !aligned(out_f32))
     return SKVQ_ERR_INVALID_ARG;
   OnDevice on(c->device);

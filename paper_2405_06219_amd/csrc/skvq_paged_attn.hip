@@ -1,6 +1,6 @@
 // skvq_paged_attention: the batch's query tokens over pages of 4-bit rows and the fp16 / bf16 rows (Eq. 1).
 //
-// A workgroup of four wavefronts takes one chunk of one sequence's tokens for one kv head and RB blocks of sixteen
+// A workgroup of four wavefronts takes some of one sequence's tokens for one kv head and RB blocks of sixteen
 // (query token, query head) rows; a wavefront takes every fourth tile of 32 tokens:
 //   scores  S^T[token][row] = K Q^T by v_mfma_f32_16x16x32_f16, two blocks of 16 tokens.  The A operand is the
 //           lane's 16 bytes of a key row: (w << 4, w, w >> 4, w >> 8) & 0x00f000f0 are its eight codes as fp16
@@ -27,8 +27,8 @@
 // and the rounded weights' own sum is taken off as often, so that only a code's distance from the middle feels the
 // rounding.  Zeros enter by fp32 sums: out = sum (w scale) code + sum w zero.
 //
-// Lengths are device data: every workgroup sums up the batch, finds the chunk size that fills the chip's workgroups
-// evenly (chunk_for) and its own units.  Bound by HBM for long contexts: 136 bytes per (token, kv head) at one group.
+// Lengths are device data: every workgroup sums up the batch's work, an equal share of it is its own, and it finds the
+// sequences that its share lies in.  Bound by HBM for long contexts: 136 bytes per (token, kv head) at one group.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -204,89 +204,93 @@ __device__ __forceinline__ V last_lane(V x) {
   return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// A sequence of the batch with its chunks, and `blocks` units' worth of query rows (none where its counts are bad).
+// A sequence of the batch with its run, and how many: `blocks` units' worth of query rows (none where its counts are bad).
 struct Member {
   Sequence s;
-  Chunks c;
+  Run run;
   int blocks;
 };
+__device__ __forceinline__ int table_capacity(const PagedLayout &L, const PagedBatch &b) {
+  const long long n = (long long)b.table_stride << L.page_log2;
+  return n < 0x7fffffff ? (int)n : 0x7fffffff;
+}
 template <int RB>
-__device__ __forceinline__ Member member_in_lane(const PagedLayout &L, const PagedBatch &b, int i, int chunk) {
+__device__ __forceinline__ Member member_in_lane(const PagedLayout &L, const PagedBatch &b, int i) {
   Member m;
   m.s = sequence_of(b, L, i < b.n_seqs ? i : b.n_seqs - 1);
   m.blocks = i < b.n_seqs && m.s.counts_ok ? (m.s.n_new * L.R + 16 * RB - 1) / (16 * RB) : 0;
   if (i >= b.n_seqs) m.s.counts_ok = true;
-  m.c = chunks_of(m.s.counts_ok ? m.s.total : 1, L.W, L.S, chunk);
+  m.run = run_of(m.s.counts_ok ? m.s.total : 1, L.W, L.S, table_capacity(L, b));
   return m;
 }
-// What a workgroup needs to know of the batch: first come the units of packed rows, sequence by sequence, then those of
-// full rows.  (Units are counted in 32 bits: the host refuses a call that could have more.)  The first 64 sequences are
-// kept in LDS, written by the first wavefront.
+// Work of all runs of a lane's sequence.  (No call has kPagedMostWork in all, the host refuses it; counts that contradict
+// each other may.)
+__device__ __forceinline__ unsigned work_in_lane(const Member &m) {
+  const unsigned long long w = (unsigned long long)m.blocks * (unsigned)(m.run.row_weight + m.run.steps);
+  return w < kPagedMostWork ? (unsigned)w : kPagedMostWork;
+}
+// What a workgroup needs to know of the batch.  The first 64 sequences are kept in LDS, written by the first wavefront.
 struct BatchPlan {
-  int chunk, packed_units, units;  // chunk size; units per kv head
-  int packed_upto, rows_upto;      // units of the sequences up to number `lane`
+  int share, work;  // a workgroup's, all (per kv head)
+  unsigned upto;    // work of the sequences up to number `lane`
 };
-__device__ __forceinline__ int units_in_lane(const Member &m, bool packed) { return m.blocks * (packed ? m.c.packed : m.c.rows); }
 template <int RB>
 __device__ __forceinline__ BatchPlan plan_batch(const PagedLayout &L, const PagedBatch &b, int groups, Member (&members)[64]) {
   const int lane = threadIdx.x & 63;
   BatchPlan p;
-  Member mine = member_in_lane<RB>(L, b, lane, kPagedMinChunk);
-  float work = 0.0f, extra = 0.0f;
-  bool bad = false;
-  Member m = mine;
-  for (int i0 = 0;;) {
+  Member m = member_in_lane<RB>(L, b, lane);
+  if (threadIdx.x < 64) members[lane] = m;
+  p.upto = lanes_up_to(work_in_lane(m));
+  unsigned work = last_lane(p.upto);
+  float about = last_lane(lanes_up_to((float)work_in_lane(m)));
+  float most = m.blocks > 0 ? (float)m.run.steps : 0.0f;  // (at most 2^24)
+  bool bad = !m.s.counts_ok;
+  for (int i0 = 64; i0 < b.n_seqs; i0 += 64) {
+    m = member_in_lane<RB>(L, b, i0 + lane);
+    work += last_lane(lanes_up_to(work_in_lane(m)));
+    about += last_lane(lanes_up_to((float)work_in_lane(m)));
+    most = fmaxf(most, m.blocks > 0 ? (float)m.run.steps : 0.0f);
     bad = bad || !m.s.counts_ok;
-    work += (float)m.blocks * m.c.nq;
-    extra += (float)m.blocks * (m.c.nq > 0);
-    if ((i0 += 64) >= b.n_seqs) break;
-    m = member_in_lane<RB>(L, b, i0 + lane, kPagedMinChunk);
+  }
+  if (about > 1.001f * kPagedMostWork) {
+    bad = true;
+    work = 0;
   }
   if (bad && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(L.errors, SKVQ_PAGED_BAD_COUNTS);
-  p.chunk = uniform(chunk_for(last_lane(lanes_up_to(work)), last_lane(lanes_up_to(extra)), groups));
-  if (p.chunk != kPagedMinChunk) mine.c = chunks_of(mine.s.counts_ok ? mine.s.total : 1, L.W, L.S, p.chunk);
-  if (threadIdx.x < 64) members[lane] = mine;
-  p.packed_upto = lanes_up_to(units_in_lane(mine, true));
-  p.rows_upto = lanes_up_to(units_in_lane(mine, false));
-  p.packed_units = last_lane(p.packed_upto);
-  p.units = last_lane(p.rows_upto);
-  for (int i0 = 64; i0 < b.n_seqs; i0 += 64) {
-    m = member_in_lane<RB>(L, b, i0 + lane, p.chunk);
-    p.packed_units += last_lane(lanes_up_to(units_in_lane(m, true)));
-    p.units += last_lane(lanes_up_to(units_in_lane(m, false)));
-  }
-  p.units += p.packed_units;
+  most = row_max(most);
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  p.work = uniform((int)work);
+  p.share = share_of(p.work, uniform((int)most), groups);
   return p;
 }
-// The unit's sequence with its chunks, its rows, its chunk (of packed or of full rows).  A chunk's row blocks are
-// neighbours: they read the same rows.
+// The run that work item `at` of the batch lies in: its sequence and rows, and how far into the run it is.
 template <int RB>
-__device__ __forceinline__ RowBlock find_unit(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, const Member (&members)[64],
-                                              int unit, Chunks &c, int &chunk, bool &packed) {
+__device__ __forceinline__ RowBlock find_run(const PagedLayout &L, const PagedBatch &b, const BatchPlan &p, const Member (&members)[64], int at,
+                                             Run &run, int &done) {
   const int lane = threadIdx.x & 63;
   RowBlock x;
-  packed = unit < p.packed_units;
-  if (!packed) unit -= p.packed_units;
-  int i0 = 0, upto = packed ? p.packed_upto : p.rows_upto;
-  while (last_lane(upto) <= unit && i0 + 64 < b.n_seqs) {  // (the unit is one of those counted)
-    unit -= last_lane(upto);
+  int i0 = 0;
+  unsigned upto = p.upto, y = (unsigned)at;
+  while (last_lane(upto) <= y && i0 + 64 < b.n_seqs) {
+    y -= last_lane(upto);
     i0 += 64;
-    upto = lanes_up_to(units_in_lane(member_in_lane<RB>(L, b, i0 + lane, p.chunk), packed));
+    upto = lanes_up_to(work_in_lane(member_in_lane<RB>(L, b, i0 + lane)));
   }
-  const unsigned long long behind = __ballot(upto > unit);
+  const unsigned long long behind = __ballot(upto > y);
   const int k = uniform(behind ? __ffsll(behind) - 1 : 63);
-  if (k > 0) unit -= __builtin_amdgcn_readlane(upto, k - 1);
+  if (k > 0) y -= (unsigned)__builtin_amdgcn_readlane((int)upto, k - 1);
   x.i = i0 + k < b.n_seqs ? i0 + k : b.n_seqs - 1;
-  const Member m = i0 ? member_in_lane<RB>(L, b, x.i, p.chunk) : members[k];  // (the same in every lane)
+  const Member m = i0 ? member_in_lane<RB>(L, b, x.i) : members[k];  // (the same in every lane)
   x.s = Sequence{uniform(m.s.row0), uniform(m.s.n_new), uniform(m.s.total), uniform(m.s.slot), true, false};
   x.s.slot_ok = x.s.slot >= 0 && x.s.slot < L.max_seqs;
-  c = Chunks{uniform(m.c.n_kept), uniform(m.c.n_win), uniform(m.c.nq), uniform(m.c.rows), uniform(m.c.packed), uniform(m.c.chunk)};
-  const int blocks = uniform(m.blocks);
-  chunk = unit;
+  run = Run{uniform(m.run.n_kept), uniform(m.run.n_win), uniform(m.run.nq), uniform(m.run.rows), uniform(m.run.row_weight), uniform(m.run.steps)};
+  done = (int)y;
   x.first = 0;
-  if (blocks > 1) {
-    chunk = unit / blocks;
-    x.first = 16 * RB * (unit - chunk * blocks);
+  if (uniform(m.blocks) > 1) {
+    const int block = done / (run.row_weight + run.steps);
+    done -= block * (run.row_weight + run.steps);
+    x.first = 16 * RB * block;
   }
   const int left = x.s.n_new * L.R - x.first;
   x.count = left < 16 * RB ? left : 16 * RB;
@@ -324,7 +328,7 @@ struct State {
   }
 };
 
-// One tile of packed rows for RB blocks of query rows.  MASKED: some of its rows are behind the chunk's end (what stands
+// One tile of packed rows for RB blocks of query rows.  MASKED: some of its rows are behind the last (what stands
 // there may be anything) or behind what some query sees.  left: rows of the tile before the end; seen: before the last one
 // that the lane's row sees.  queries(r, j): block r's B operand for key dwords j; alpha: on the scores, with the code's unit.
 template <class T, int NG, int FMT, int RB, bool MASKED, class Q, class Next>
@@ -470,7 +474,7 @@ __device__ __forceinline__ int last_token(const PagedLayout &L, const RowBlock &
   return x.s.total - x.s.n_new + quotient(x.first + (row < x.count ? row : x.count - 1), L.recip_R);
 }
 
-// Pages of the wavefront's tiles k0 .. k0 + 31 of a chunk [begin, end) of packed rows, two blocks of 16 tokens each: lane
+// Pages of the wavefront's tiles k0 .. k0 + 31 of packed rows begin .. end - 1, two blocks of 16 tokens each: lane
 // 2k + i holds tile k0 + k's block i.
 __device__ __forceinline__ int pages_of_tiles(const PagedLayout &L, const PagedBatch &b, int seq, int begin, int end, int k0, bool &bad) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -487,15 +491,14 @@ __device__ __forceinline__ int pages_of_tiles(const PagedLayout &L, const PagedB
   return id;
 }
 
-// The wavefront's share of a chunk of packed rows.  ids: pages_of_tiles of its first tiles.
+// The wavefront's share of packed rows begin .. end - 1.  ids: pages_of_tiles of its first tiles.
 template <class T, int NG, int FMT, int RB>
-__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T, RB> &lds, const RowBlock &x, const Chunks &ch,
-                                            int chunk, int h, int ids, State<NG> (&st)[RB], bool &bad) {
+__device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBatch &b, const Lds<T, RB> &lds, const RowBlock &x, int begin, int end,
+                                            int h, int ids, State<NG> (&st)[RB], bool &bad) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   int seen[RB];  // packed rows that the lane's row sees; all rows see the first one's
 #pragma unroll
   for (int r = 0; r < RB; ++r) seen[r] = last_token(L, x, 16 * r + c) + 1 - L.S;
-  const int begin = chunk * ch.chunk, end = min(ch.nq, begin + ch.chunk);
   const int all_see = min(end, last_token(L, x, 0) + 1 - L.S);
   const int n_tiles = (end - begin + kTile - 1) / kTile, mine = n_tiles > wave ? (n_tiles - wave + kWaves - 1) / kWaves : 0;
   const uint8_t *head_part = L.pages + (long long)h * L.part_bytes;
@@ -586,7 +589,7 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
       for (int n = 1; n < NG; ++n) qs[r][0] = g == n ? qs[r][n] : qs[r][0];
     }
   }
-  // Whole tiles that every query sees, then the others (at the chunk's end).  The lanes hold the pages of 32 tiles, and the
+  // Whole tiles that every query sees, then the others (at the end).  The lanes hold the pages of 32 tiles, and the
   // next tile's pairs, key codes and value codes are asked for as soon as this one's have been used (the last one's loads are
   // repeated: no branch between loads and what they hide behind): 31 tiles a turn.
   const int whole_tiles = all_see > begin ? (all_see - begin) / kTile : 0;
@@ -607,15 +610,14 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
   }
 }
 
-// ... of a chunk of full-precision rows: the u-th of the kept and the ring tokens, in the order of their numbers.
+// ... of full-precision rows: the u-th of the kept and the ring tokens, in the order of their numbers.
 template <class T, int NG, int RB>
-__device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T, RB> &lds, const RowBlock &x, const Chunks &ch, int chunk, int h,
-                                          int block, State<NG> &st) {
+__device__ __forceinline__ void take_rows(const PagedLayout &L, const Lds<T, RB> &lds, const RowBlock &x, const Run &ch, int begin, int end,
+                                          int h, int block, State<NG> &st) {
   typedef T t8 __attribute__((ext_vector_type(8)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int last = last_token(L, x, 16 * block + c);
   const float scale = L.sm_scale * kLog2e;
-  const int n_full = ch.n_kept + ch.n_win, begin = chunk * kPagedRowsPerChunk, end = min(n_full, begin + kPagedRowsPerChunk);
   const long long head = ((long long)x.s.slot * L.Hk + h) * (L.W + L.S) * kD;
   const T *k_rows = reinterpret_cast<const T *>(L.k_rows) + head, *v_rows = reinterpret_cast<const T *>(L.v_rows) + head;
   const int first_recent = x.s.total - ch.n_win, first_slot = first_recent % L.W;
@@ -685,11 +687,17 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
   const int p = threadIdx.x % kD, packed_channel = L.v_offset[h * kD + 8 * (p & 15) + (p >> 4)] / 2;  // of the output place it writes
   const BatchPlan plan = plan_batch<RB>(L, b, gridDim.y, lds.members);
   __syncthreads();
-  for (int unit = blockIdx.y; unit < plan.units; unit += gridDim.y) {
-    int chunk;
-    bool packed;
-    Chunks ch;
-    const RowBlock x = find_unit<RB>(L, b, plan, lds.members, unit, ch, chunk, packed);
+  const long long mine_from = (long long)plan.share * blockIdx.y;
+  const int stop = (int)min((long long)plan.work, mine_from + plan.share);
+  int next = 0;
+  for (int at = (int)min(mine_from, (long long)plan.work); at < stop; at += next) {
+    Run run;
+    int done;
+    const RowBlock x = find_run<RB>(L, b, plan, lds.members, at, run, done);
+    const Portion part = portion_of(run, done, at, stop, plan.share);
+    next = part.work;
+    if (!part.there) continue;
+    const bool packed = part.packed;
     // the queries, sixteen threads a row, rows past the last one repeat it; the first pages meanwhile
     static_assert(64 * kWaves == 16 * 16, "one piece of a row per thread");
     const int query = threadIdx.x >> 4;
@@ -699,13 +707,9 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
       const QueryRow from = query_row(L, x, h, min(16 * r + query, x.count - 1));
       mine[r] = *reinterpret_cast<const P *>((const T *)q.p + from.token * q.stride + from.head * kD + 8 * c);
     }
-    bool bad = false;
-    int ids = 0;
-    if (packed) {
-      const int begin = chunk * ch.chunk;
-      ids = pages_of_tiles(L, b, x.i, begin, min(ch.nq, begin + ch.chunk), 0, bad);
-    }
-    __syncthreads();  // (the unit before has read its partials out of LDS)
+    bool bad = run.nq > table_capacity(L, b);
+    const int ids = packed ? pages_of_tiles(L, b, x.i, part.begin, part.end, 0, bad) : 0;
+    __syncthreads();  // (the portion before has read its partials out of LDS)
     if (threadIdx.x == 0) {
       lds.bad = !x.s.slot_ok;
       if (!x.s.slot_ok) atomicOr(L.errors, SKVQ_PAGED_BAD_SLOT);
@@ -741,14 +745,14 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
 #pragma unroll
     for (int r = 0; r < RB; ++r) st[r].clear();
     if (packed) {
-      take_packed<T, NG, FMT, RB>(L, b, lds, x, ch, chunk, h, ids, st, bad);
+      take_packed<T, NG, FMT, RB>(L, b, lds, x, part.begin, part.end, h, ids, st, bad);
     } else if (x.s.slot_ok) {
 #pragma unroll
-      for (int r = 0; r < RB; ++r) take_rows<T, NG, RB>(L, lds, x, ch, chunk, h, r, st[r]);
+      for (int r = 0; r < RB; ++r) take_rows<T, NG, RB>(L, lds, x, run, part.begin, part.end, h, r, st[r]);
     }
 
     // The wavefronts' states: sums over the lanes of a row, then one reference for the workgroup.
-    const int n_partials = ch.rows + ch.packed, most = kPagedMaxSplits + n_row_chunks;
+    const int most = kPagedMaxSplits + n_row_chunks;
     const int channel = packed ? packed_channel : p;
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
@@ -800,17 +804,17 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
         if (lds.bad) l = NAN;
         const QueryRow qr = query_row(L, x, h, 16 * r + row);
         float *to = L.workspace + ((long long)qr.token * L.Hq + qr.head) * most * kPartialStride;
-        if (n_partials == 1) {
+        if (part.n_partials == 1) {
           store_out<T>(L, out, qr, channel, acc / l);
         } else {
-          float *part = to + (packed ? ch.rows + chunk : chunk) * kPartialStride;
-          part[4 + channel] = acc;
+          float *mine_to = to + part.partial * kPartialStride;
+          mine_to[4 + channel] = acc;
           if (p == 0) {
-            part[0] = m;
-            part[1] = l;
+            mine_to[0] = m;
+            mine_to[1] = l;
           }
         }
-        if (p == 0 && !packed && chunk == 0) to[2] = __uint_as_float((unsigned)n_partials);  // (for the merge)
+        if (p == 0 && part.partial == 0) to[2] = __uint_as_float((unsigned)part.n_partials);  // (for the merge)
       }
     }
   }
@@ -827,7 +831,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
   const QueryRow qr = {token, (int)blockIdx.y};
   const float *from = L.workspace + ((long long)token * L.Hq + qr.head) * (kPagedMaxSplits + n_row_chunks) * kPartialStride;
   auto partial = [&](int i) { return from + (long long)i * kPartialStride; };
-  const int n = (int)__float_as_uint(from[2]);  // (anything where the token is of no sequence)
+  // (anything where the token is of no sequence, or nothing was done)
+  const int n = min((int)__float_as_uint(from[2]), kPagedMaxSplits + n_row_chunks);
   const Sequence s = sequence_of(b, L, sequence_of_unit(b, token, kTokenDeal));
   if (!s.counts_ok || token < s.row0 || token >= s.row0 + s.n_new || n <= 1) return;
   float m = kNothing, l = 0.0f;
@@ -900,21 +905,25 @@ hipError_t launch_typed(const PagedLayout &L, const PagedBatch &b, TokenRows q, 
 
 }  // namespace
 
+static int row_blocks_of(long long rows, int n_seqs) { return rows > 16LL * n_seqs ? 2 : 1; }
+
+long long paged_most_work(const PagedLayout &L, const skvq_batch &b) {
+  const long long rows = (long long)b.n_tokens * L.R, capacity = (long long)b.table_stride << L.page_log2;
+  const long long blocks = rows / (16 * row_blocks_of(rows, b.n_seqs)) + (b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens);
+  return blocks * (row_weight_of(L.W + L.S) + (capacity < 0x7fffffff ? steps_of((int)capacity, kPagedStep) : 1 << 24));
+}
+
 hipError_t launch_paged_attention(const PagedLayout &L, const skvq_batch &batch, TokenRows q, void *out, long long out_stride,
                                   float *out_f32, int n_cus, hipStream_t s) {
   const PagedBatch b = batch_of(batch);
   const int row_chunks = paged_row_chunks(L.W, L.S);
   // Lengths are not known here: as many workgroups as the chip holds at once, over the kv heads, unless there can be no
-  // more units than that (every query token of a sequence of its own, as long as the page table allows).  Where a sequence
+  // more work than that (every query token of a sequence of its own, as long as the page table allows).  Where a sequence
   // has more than 16 rows per kv head on average, a unit holds two blocks of them.
-  const long long rows = (long long)b.n_tokens * L.R;
-  const int row_blocks = rows > 16LL * b.n_seqs ? 2 : 1;
-  const long long blocks = rows / (16 * row_blocks) + (b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens);
-  long long splits = ((long long)b.table_stride << L.page_log2) / kPagedMinChunk + 1;
-  if (splits > kPagedMaxSplits) splits = kPagedMaxSplits;
-  const long long units = blocks * (row_chunks + splits), most = (long long)groups_per_cu(L.NG, row_blocks) * n_cus / L.Hk;
-  if (units > 1 << 30) return hipErrorInvalidValue;  // (counted in 32 bits)
-  const unsigned groups = (unsigned)(units < most ? units : most > 0 ? most : 1);
+  const long long work = paged_most_work(L, batch), rows = (long long)b.n_tokens * L.R;
+  const int row_blocks = row_blocks_of(rows, b.n_seqs);
+  const long long shares = work / kPagedMinShare + 1, most = (long long)groups_per_cu(L.NG, row_blocks) * n_cus / L.Hk;
+  const unsigned groups = (unsigned)(shares < most ? shares : most > 0 ? most : 1);
   const Out o{out, out_stride, out_f32};
   if (L.dtype == SKVQ_DTYPE_BF16)
     return row_blocks == 2 ? launch_typed<__bf16, 2>(L, b, q, o, row_chunks, groups, s) : launch_typed<__bf16, 1>(L, b, q, o, row_chunks, groups, s);

@@ -80,48 +80,74 @@ constexpr TokenPlace token_place(int token, int total, int W, int S) {
   return token >= total - W ? TokenPlace{true, token % W} : token < S ? TokenPlace{true, W + token} : TokenPlace{false, token - S};
 }
 
-// Attention: the rows of a sequence are cut into chunks of full-precision rows and chunks of packed rows, each read by a
-// workgroup per (block of 16 query rows, kv head): a unit.  A workgroup's wavefronts take every kPagedWaves-th tile of a
-// chunk of packed rows; chunks are whole tiles for each of them, at least two.
+// Attention: work is counted in steps of packed rows (a tile for each of a workgroup's wavefronts) and dealt out in equal
+// shares.  A run, one unit's query rows of a sequence against all it sees, is its chunks of full-precision rows (each taken
+// whole by the workgroup in whose share it begins; 128 rows count as four steps, by their bytes) and then its steps of
+// packed rows.  Runs follow one another; a share may end in one run and begin in another, and what each workgroup finds of
+// a run is a partial result.
 constexpr int kPagedWaves = 4, kPagedTile = 32;
 constexpr int kPagedStep = kPagedTile * kPagedWaves;
-constexpr int kPagedMinChunk = 2 * kPagedStep;
-constexpr int kPagedMaxSplits = 128;     // chunks of packed rows of a sequence
+constexpr int kPagedMaxSplits = 128;     // partial results of packed rows of a run
 constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
+constexpr int kRowStep = 128, kRowStepWeight = 4, kRowChunkWeight = kPagedRowsPerChunk / kRowStep * kRowStepWeight;
+constexpr int kPagedMinShare = 2;
+constexpr unsigned kPagedMostWork = 1u << 30;  // of a call: work is counted in 32 bits
 constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
-constexpr int whole_steps(int rows) { return (rows / kPagedStep + (rows % kPagedStep > 0)) * kPagedStep; }
-// Lengths are known on the device only, so every workgroup, of `groups` per kv head, finds the batch's chunk size from two
-// sums over the batch: `work`, packed rows times blocks, and `extra`, units beyond work / chunk at most (a last, shorter
-// chunk per block).  The units of packed rows fit `rounds` rounds over the groups of a head: as few as keep a chunk within
-// 4096 rows, more where the extra units would fill half of them.  (The units of full rows, short ones, come after them.
-// Numbers of 24 bits do: units are counted exactly from the chunk size, which is the same in every workgroup.)
-constexpr int chunk_for(float work, float extra, int groups) {
-  const float least = work / (4096.0f * groups), full = 2.0f * extra / groups;
-  const float most = least > full ? least : full;
-  const float rounds = (float)(int)(most < 1e6f ? most : 1e6f) + 1.0f;
-  const float rows = work / (rounds * groups - extra);  // (positive: rounds > full)
-  const int chunk = whole_steps(rows < 1e9f ? (int)rows + 1 : 1000000000);
-  return chunk < kPagedMinChunk ? kPagedMinChunk : chunk;
+constexpr int steps_of(int rows, int step) { return rows / step + (rows % step > 0); }
+constexpr int row_weight_of(int rows) { return kRowStepWeight * steps_of(rows, kRowStep); }
+struct Run {
+  int n_kept, n_win, nq;  // sink rows, ring rows, packed rows
+  int rows, row_weight;   // chunks of full rows, their work
+  int steps;              // of packed rows
+};
+// capacity: packed rows that a row of the page table has room for (a longer sequence is an error, found elsewhere).
+constexpr Run run_of(int total, int W, int S, int capacity) {
+  Run r{0, total < W ? total : W, 0, 0, 0, 0};
+  const int before = total - r.n_win;
+  r.n_kept = before < S ? before : S;
+  r.nq = before - r.n_kept;
+  r.rows = (r.n_win + r.n_kept + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk;
+  r.row_weight = row_weight_of(r.n_win + r.n_kept);
+  r.steps = steps_of(r.nq < capacity ? r.nq : capacity, kPagedStep);
+  return r;
+}
+// The share of each of `groups` workgroups (of a kv head), with room for a run's partial results.
+constexpr int share_of(int work, int most_steps, int groups) {
+  int share = steps_of(work, groups);
+  const int least = steps_of(most_steps, kPagedMaxSplits - 2);
+  if (least > share) share = least;
+  return share < kPagedMinShare ? kPagedMinShare : share;
+}
+// What a workgroup does next: its share ends at `stop`, it is at `at`, which is `done` into the run.
+struct Portion {
+  int work;                 // how far it goes, at least 1
+  bool there, packed;       // !there: the rest of a chunk that another workgroup has
+  int begin, end;           // rows
+  int partial, n_partials;  // which of the run's partial results, of how many
+};
+constexpr Portion portion_of(const Run &r, int done, int at, int stop, int share) {
+  const int packed_at = at - done + r.row_weight, first = packed_at / share;
+  Portion p{1, true, done >= r.row_weight, 0, 0, 0, r.rows + (r.steps > 0 ? (packed_at + r.steps - 1) / share - first + 1 : 0)};
+  if (p.packed) {
+    const int step = done - r.row_weight, left = r.steps - step, n = stop - at < left ? stop - at : left;
+    if (n > 0) p.work = n;
+    p.begin = step * kPagedStep;
+    const long long end = (long long)(step + p.work) * kPagedStep;
+    p.end = end < r.nq ? (int)end : r.nq;
+    p.partial = r.rows + at / share - first;
+  } else {
+    p.partial = done / kRowChunkWeight;
+    p.there = done % kRowChunkWeight == 0;
+    const int next = (p.partial + 1) * kRowChunkWeight;
+    p.work = (next < r.row_weight ? next : r.row_weight) - done;
+    p.begin = p.partial * kPagedRowsPerChunk;
+    p.end = p.begin + kPagedRowsPerChunk < r.n_kept + r.n_win ? p.begin + kPagedRowsPerChunk : r.n_kept + r.n_win;
+  }
+  return p;
 }
 // Quotient by a number of 1 .. 16 (recip_of it) of y < 2^27.
 constexpr unsigned recip_of(int divisor) { return ((1u << 31) + divisor - 1) / divisor; }
 constexpr int quotient(int y, unsigned recip) { return (int)(((unsigned long long)(2u * (unsigned)y) * recip) >> 32); }
-struct Chunks {
-  int n_kept, n_win, nq;    // sink rows, ring rows, packed rows
-  int rows, packed, chunk;  // chunks of full rows, of packed rows; packed rows per chunk
-};
-constexpr Chunks chunks_of(int total, int W, int S, int chunk) {
-  Chunks c{0, total < W ? total : W, 0, 0, 0, chunk};
-  const int before = total - c.n_win;
-  c.n_kept = before < S ? before : S;
-  c.nq = before - c.n_kept;
-  c.rows = (c.n_win + c.n_kept + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk;
-  const int least = whole_steps(c.nq / kPagedMaxSplits + (c.nq % kPagedMaxSplits > 0));  // (partials have room for so many)
-  if (least > c.chunk) c.chunk = least;
-  c.packed = c.nq / c.chunk + (c.nq % c.chunk > 0);
-  return c;
-}
-
 // Whether a sequence's entry x of the page table can be followed.
 constexpr bool page_known(int x, int table_stride) { return x >= 0 && x < table_stride; }
 constexpr bool page_valid(int id, int n_pages) { return id >= 0 && id < n_pages; }

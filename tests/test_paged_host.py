@@ -41,11 +41,32 @@ extern "C" int place(int token, int total, int W, int S) {
   const TokenPlace p = token_place(token, total, W, S);
   return p.full ? -1 - p.row : p.row;
 }
-extern "C" int chunk_size(float work, float extra, int groups) { return chunk_for(work, extra, groups); }
 extern "C" int divided(int y, int by) { return quotient(y, recip_of(by)); }
-extern "C" void chunks(int total, int W, int S, int chunk, int *out) {
-  const Chunks c = chunks_of(total, W, S, chunk);
-  out[0] = c.n_kept; out[1] = c.n_win; out[2] = c.nq; out[3] = c.rows; out[4] = c.packed; out[5] = c.chunk;
+extern "C" void run(int total, int W, int S, int capacity, int *out) {
+  const Run r = run_of(total, W, S, capacity);
+  out[0] = r.n_kept; out[1] = r.n_win; out[2] = r.nq; out[3] = r.rows; out[4] = r.row_weight; out[5] = r.steps;
+}
+extern "C" int share(int work, int most_steps, int groups) { return share_of(work, most_steps, groups); }
+// The portions of workgroups 0 .. groups - 1 in runs one after another: {run, work, there, packed, begin, end, partial, n_partials}.
+extern "C" int portions(int n, const int *totals, int W, int S, int groups, int share, int *out, int most) {
+  long long work = 0;
+  for (int i = 0; i < n; ++i) { const Run r = run_of(totals[i], W, S, 0x7fffffff); work += r.row_weight + r.steps; }
+  int k = 0;
+  for (int g = 0; g < groups; ++g) {
+    const long long from = (long long)g * share;
+    const int stop = (int)(work < from + share ? work : from + share);
+    for (int at = (int)(work < from ? work : from); at < stop;) {
+      int i = 0, done = at;
+      Run r = run_of(totals[0], W, S, 0x7fffffff);
+      while (done >= r.row_weight + r.steps) { done -= r.row_weight + r.steps; r = run_of(totals[++i], W, S, 0x7fffffff); }
+      const Portion p = portion_of(r, done, at, stop, share);
+      if (k == most) return -1;
+      int *o = out + 8 * k++;
+      o[0] = i; o[1] = p.work; o[2] = p.there; o[3] = p.packed; o[4] = p.begin; o[5] = p.end; o[6] = p.partial; o[7] = p.n_partials;
+      at += p.work;
+    }
+  }
+  return k;
 }
 extern "C" int page_ok(int x, int stride, int id, int n_pages) { return page_known(x, stride) && page_valid(id, n_pages); }
 """
@@ -132,42 +153,51 @@ def test_read_covers_its_tokens_once(plan):
             assert plan.place(a, total, W, S) == want
 
 
-def test_chunks_cover_all_rows(plan):
+def test_runs(plan):
     out = np.zeros(6, np.int32)
     for total in [1, 2, 127, 128, 129, 133, 134, 384, 385, 700, 4000, 131072, 2 ** 24 + 7, 2 ** 31 - 65]:
         for W, S in [(1, 0), (128, 0), (128, 5), (600, 1000), (1 << 20, 1 << 20)]:
-            for least in [256, 384, 4096, 2 ** 30]:
-                plan.chunks(total, W, S, least, out.ctypes.data_as(C.c_void_p))
-                kept, win, nq, rows, packed, chunk = (int(x) for x in out)
+            for capacity in [0, 256, 4096, 2 ** 31 - 1]:
+                plan.run(total, W, S, capacity, out.ctypes.data_as(C.c_void_p))
+                kept, win, nq, rows, weight, steps = (int(x) for x in out)
                 assert win == min(total, W) and kept == min(total - win, S) and kept + win + nq == total
-                assert rows == -(-(kept + win) // 512) and packed == -(-nq // chunk) <= 128
-                assert chunk % 128 == 0 and chunk >= least
+                assert rows == -(-(kept + win) // 512) and weight == 4 * -(-(kept + win) // 128)
+                assert steps == -(-min(nq, capacity) // 128)
 
 
 @pytest.mark.parametrize("groups", [1, 24, 96, 768])
-def test_units_fill_rounds_of_the_workgroups(plan, groups):
-    """The chunk size that the device finds: the batch's units of packed rows fit whole rounds over the workgroups."""
+def test_shares_cover_every_run_once(plan, groups):
+    """Every row of every run is in one portion, partial results are numbered without gaps and fit the workspace, and no
+    workgroup has more than its share and what a chunk of full rows goes past its end."""
     rng = np.random.default_rng(groups)
-    out = np.zeros(6, np.int32)
-    plan.chunk_size.argtypes = [C.c_float, C.c_float, C.c_int]
-    for trial in range(300):
-        W, S = int(rng.choice([1, 128, 700])), int(rng.choice([0, 5]))
+    room = np.zeros((100000, 8), np.int32)
+    for trial in range(120):
+        W, S = int(rng.choice([1, 128, 700, 3000])), int(rng.choice([0, 5, 900]))
         lens = [int(10 ** rng.uniform(0, rng.uniform(1, 5.5))) for _ in range(rng.integers(1, 80))]
-        blocks = [int(rng.choice([0, 1, 1, 1, 4])) for _ in lens]
-
-        def chunks(total, least):
-            plan.chunks(total, W, S, least, out.ctypes.data_as(C.c_void_p))
-            return [int(x) for x in out]
-        got = [chunks(t, 256) for t in lens]
-        work = sum(b * c[2] for b, c in zip(blocks, got))
-        extra = sum(b * (c[2] > 0) for b, c in zip(blocks, got))
-        size = plan.chunk_size(work, extra, groups)
-        assert size % 128 == 0 and size >= 256
-        rounds = max(work / (4096 * groups), 2 * extra / groups) * (1 + 1e-6) // 1 + 1
-        units = sum(b * c[4] for b, c in zip(blocks, [chunks(t, size) for t in lens]))
-        assert units <= rounds * groups
-    assert plan.chunk_size(0, 0, groups) == 256
-    assert plan.chunk_size(2.0 ** 62, 2.0 ** 40, groups) >= 256
+        runs = []
+        for t in lens:
+            out = np.zeros(6, np.int32)
+            plan.run(t, W, S, 2 ** 31 - 1, out.ctypes.data_as(C.c_void_p))
+            runs.append([int(x) for x in out])
+        work = sum(r[4] + r[5] for r in runs)
+        share = plan.share(work, max(r[5] for r in runs), groups)
+        assert share >= 2 and share * groups >= work
+        totals = np.array(lens, np.int32)
+        n = plan.portions(len(lens), totals.ctypes.data_as(C.c_void_p), W, S, groups, share, room.ctypes.data_as(C.c_void_p), len(room))
+        assert n > 0
+        got = room[:n].copy()
+        assert got[:, 1].min() >= 1 and got[got[:, 3] == 1][:, 1].max(initial=0) <= share
+        for i, (kept, win, nq, rows, weight, steps) in enumerate(runs):
+            mine = got[(got[:, 0] == i) & (got[:, 2] == 1)]
+            packed, full = mine[mine[:, 3] == 1], mine[mine[:, 3] == 0]
+            for part, count in ((packed, nq), (full, kept + win)):
+                assert sorted(map(tuple, part[:, 4:6])) == list(map(tuple, part[:, 4:6]))
+                ends = np.concatenate([[0], part[:, 5]])
+                assert (part[:, 4] == ends[:-1]).all() and ends[-1] == count
+            assert sorted(mine[:, 6]) == list(range(len(mine))) and (mine[:, 7] == len(mine)).all()
+            assert (full[:, 6] < rows).all() and len(packed) <= 127 and (packed[:, 4] % 128 == 0).all()
+    assert plan.share(0, 0, groups) == 2
+    assert plan.share(2 ** 30 - 1, 2 ** 24, groups) >= 2 ** 24 // 126
 
 
 def test_quotients(plan):
