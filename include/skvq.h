@@ -533,9 +533,12 @@ int skvq_paged_read(skvq_paged *cache, const skvq_batch *batch, void *k, int64_t
 /* Eq. 1 for the batch's query tokens, each over the tokens of its sequence up to and including itself, in the
  * form they are stored in now: query j of n_i new tokens sees tokens 0 .. seq_lens[i] - n_i + j.
  * q: DEVICE [n_tokens][Hq][D], rotated as the keys are; out: likewise, in the cache's type, or NULL; out_f32: DEVICE
- * fp32 [n_tokens][Hq][D] contiguous, or NULL (not both).  Scores and sums in fp32; softmax weights enter the
- * value product as fp16 numbers (half a step of 2^-11 each; bf16 rows as two bf16 parts).
- * SKVQ_ERR_INVALID_ARG if n_tokens > max_tokens. */
+ * fp32 [n_tokens][Hq][D] contiguous, or NULL (not both).  Scores and sums in fp32; a softmax weight enters
+ * the value product as two fp16 parts (F16 caches) or one, half a step of 2^-11 on what it adds to the middle
+ * code (BF16 caches); of full-precision rows as two parts of the cache's type.  An infinity or NaN among the
+ * new tokens' values also reaches the call's earlier query tokens of that sequence (0 times it is NaN).
+ * SKVQ_ERR_INVALID_ARG if n_tokens > max_tokens.  SKVQ_ERR_UNSUPPORTED if n_tokens * Hq / Hk >= 2^27, or if
+ * (16 query rows) x (128 tokens of table_stride * P) could come to 2^30 and more pieces of work. */
 int skvq_paged_attention(skvq_paged *cache, const skvq_batch *batch, const void *q, int64_t q_stride, void *out,
                          int64_t out_stride, float *out_f32, void *hip_stream);
 

@@ -404,6 +404,31 @@ def test_refusals_of_calls(B):
     b.check_buffers()
 
 
+def test_a_call_of_more_work_than_is_counted_is_refused(B):
+    b = Both(B, hq=16, hk=1, max_tokens=128, page=256, n_pages=8, max_seqs=1, seed=31)
+    q = b.draw(128, 16).to(DEV)
+    wide = torch.zeros((1, 2 ** 23), dtype=torch.int32, device=DEV)      # 2^31 tokens of a sequence: 2^24 steps
+    batch = B.SkvqBatch(ints([0, 128]), ints([128]), wide, n_tokens=128)  # 2048 query rows: 64 pairs of blocks
+    with pytest.raises(B.SkvqError) as e:
+        b.gpu.skvq_paged_attention(batch, q)
+    assert e.value.status == B.SKVQ_ERR_UNSUPPORTED
+
+
+def test_counts_that_contradict_each_other(B):
+    """A sequence of a negative count between two good ones that overlap: it is left out, the error is noted, and the two
+    others' rows are theirs (the later of two that write one row may be either)."""
+    b = Both(B, seed=32, max_tokens=8)
+    b.append([0, 1, 2, 3], [30, 40, 50, 60])
+    q = b.draw(4, 4)
+    batch = B.SkvqBatch(ints([0, 2, 1, 4]), ints([30, 40, 50]), ints(b.table[:3]), slots=ints(b.slots[:3]), n_tokens=4)
+    got = b.gpu.skvq_paged_attention(batch, q.to(DEV)).double().cpu().numpy()
+    assert b.gpu.skvq_paged_errors() == B.SKVQ_PAGED_BAD_COUNTS
+    for rows, i, n in ((slice(0, 1), 0, 2), (slice(2, 4), 2, 3)):
+        want, bound = b.plain.attend(int(b.slots[i]), q[(0 if i == 0 else 1):(2 if i == 0 else 4)].float().numpy(), None)
+        own = slice(0, 1) if i == 0 else slice(1, 3)
+        assert (np.abs(got[rows] - want[own]) <= bound[own]).all()
+
+
 def test_another_stream_and_the_same_bits_every_time(B):
     b = Both(B, hq=8, hk=2, n_pages=400, page=16, max_seqs=2, window=32, seed=19)
     b.append([0, 1], [2500, 700])
