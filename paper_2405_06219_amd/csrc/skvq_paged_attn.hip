@@ -16,8 +16,7 @@
 // load, conversion and logarithm per tile and group, and every use reads them by a lane broadcast.  What a tile's pairs, key
 // codes and value codes leave free, the next tile's take in the same registers (a second buffer is 26 registers at four
 // groups and hides no more: HBM answers within half a tile's work).
-// Work on vectors bounds calls of many rows per kv head: two blocks share unpacking and broadcasts (RB = 2), which takes
-// eight sequences of up to 40k tokens with two to eight new ones, four fp32 groups, from 119 to 115 us.
+// Work on vectors bounds calls of many rows per kv head: two blocks share unpacking and broadcasts (RB = 2).
 //
 // The weight that multiplies a code is weight * scale: the reference counts log2 of the largest scale at hand in, so
 // that this product stays within fp16's normal numbers near the largest contributions.  For fp16 outputs it is taken in
@@ -905,6 +904,9 @@ hipError_t launch_typed(const PagedLayout &L, const PagedBatch &b, TokenRows q, 
 
 }  // namespace
 
+// Two blocks a unit where sequences have more than 16 rows on average (us with one -> two, 8 kv heads): 8 sequences of 40k
+// tokens with 64 rows each, one group 258 -> 209, two 257 -> 198, four 312 -> 269, with 20 rows 139 -> 123; 1024 rows of a
+// sequence of 32k 343 -> 310.  With 16 rows at most the second block would be idle.
 static int row_blocks_of(long long rows, int n_seqs) { return rows > 16LL * n_seqs ? 2 : 1; }
 
 long long paged_most_work(const PagedLayout &L, const skvq_batch &b) {
@@ -922,8 +924,8 @@ hipError_t launch_paged_attention(const PagedLayout &L, const skvq_batch &batch,
   // has more than 16 rows per kv head on average, a unit holds two blocks of them.
   const long long work = paged_most_work(L, batch), rows = (long long)b.n_tokens * L.R;
   const int row_blocks = row_blocks_of(rows, b.n_seqs);
-  const long long shares = work / kPagedMinShare + 1, most = (long long)groups_per_cu(L.NG, row_blocks) * n_cus / L.Hk;
-  const unsigned groups = (unsigned)(shares < most ? shares : most > 0 ? most : 1);
+  const long long most = (long long)groups_per_cu(L.NG, row_blocks) * n_cus / L.Hk;
+  const unsigned groups = (unsigned)(work < most ? work : most > 0 ? most : 1);
   const Out o{out, out_stride, out_f32};
   if (L.dtype == SKVQ_DTYPE_BF16)
     return row_blocks == 2 ? launch_typed<__bf16, 2>(L, b, q, o, row_chunks, groups, s) : launch_typed<__bf16, 1>(L, b, q, o, row_chunks, groups, s);

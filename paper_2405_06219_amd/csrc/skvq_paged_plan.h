@@ -90,7 +90,6 @@ constexpr int kPagedStep = kPagedTile * kPagedWaves;
 constexpr int kPagedMaxSplits = 128;     // partial results of packed rows of a run
 constexpr int kPagedRowsPerChunk = 512;  // rows of k_rows / v_rows per chunk
 constexpr int kRowStep = 128, kRowStepWeight = 4, kRowChunkWeight = kPagedRowsPerChunk / kRowStep * kRowStepWeight;
-constexpr int kPagedMinShare = 2;
 constexpr unsigned kPagedMostWork = 1u << 30;  // of a call: work is counted in 32 bits
 constexpr int paged_row_chunks(int W, int S) { return (W + S + kPagedRowsPerChunk - 1) / kPagedRowsPerChunk; }
 constexpr int steps_of(int rows, int step) { return rows / step + (rows % step > 0); }
@@ -116,7 +115,7 @@ constexpr int share_of(int work, int most_steps, int groups) {
   int share = steps_of(work, groups);
   const int least = steps_of(most_steps, kPagedMaxSplits - 2);
   if (least > share) share = least;
-  return share < kPagedMinShare ? kPagedMinShare : share;
+  return share > 0 ? share : 1;
 }
 // What a workgroup does next: its share ends at `stop`, it is at `at`, which is `done` into the run.
 struct Portion {
