@@ -172,6 +172,39 @@ def test_long_contexts(B, dtype, group):
     b.check_attention([0, 1], [2, 1])
 
 
+@pytest.mark.parametrize("window,sinks", [(1100, 0), (600, 700), (512, 512)])
+def test_full_rows_of_several_chunks(B, window, sinks):
+    b = Both(B, hq=6, hk=2, window=window, sinks=sinks, page=32, n_pages=64, max_seqs=4, max_tokens=40, seed=33)
+    seqs, held = [3, 1, 0, 2], [window + sinks + 400, 513, 1, window + 3]
+    b.append(seqs, held)
+    b.check_attention(seqs, [1, 1, 1, 1])
+    b.check_attention(seqs, [20, 7, 1, 12])
+
+
+def test_more_partial_results_than_threads(B):
+    """A window of 139000 rows is 272 chunks.  Against the formula in 64 bits on the device; the bound: half a step of the
+    output, 2^-20 of the largest possible sum for weights (two parts) and sums, and scores' fp32 products and logarithms,
+    2^-21 of their terms' sizes, on the distance of the values from the output."""
+    n, W = 139000, 140000
+    rng = torch.Generator(device=DEV).manual_seed(7)
+    perm = np.arange(D, dtype=np.int32)[None]
+    cache = B.SkvqPagedCache(2, 1, 128, W, 16, 4, 1, 1, perm, perm, np.ones((1, 1), np.float32), np.ones((1, 1), np.float32), device=DEV)
+    k, v = (torch.randn((n, 1, D), generator=rng, device=DEV).half() for _ in range(2))
+    q = torch.randn((1, 2, D), generator=rng, device=DEV).half()
+    table = torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    cache.skvq_paged_append(B.SkvqBatch(ints([0, n]), ints([n]), table, n_tokens=n), k, v)
+    got = cache.skvq_paged_attention(B.SkvqBatch(ints([0, 1]), ints([n]), table, n_tokens=1), q)[0].double()
+    assert cache.skvq_paged_errors() == 0
+    x, y = k[:, 0].double(), v[:, 0].double()
+    for r in range(2):
+        scores = (x * q[0, r].double()).sum(1) / D ** 0.5
+        p = torch.softmax(scores, 0)[:, None]
+        want = (p * y).sum(0)
+        size = (x.abs() * q[0, r].double().abs()).sum(1, keepdim=True) / D ** 0.5
+        bound = 2.0 ** -11 * want.abs() + 2.0 ** -20 * (p * y.abs()).sum(0) + 2.0 ** -21 * (p * size * (y - want).abs()).sum(0) + 2.0 ** -25
+        assert bool(((got[r] - want).abs() <= bound).all()), float(((got[r] - want).abs() / bound).max())
+
+
 def test_values_without_spread_and_scores_far_apart(B):
     # a scale of zero has no logarithm; one token takes all the weight, first, last or packed; the largest fp16 queries
     b = Both(B, hq=2, hk=1, window=4, page=16, n_pages=16, max_seqs=1, seed=9, meta="f32")
