@@ -21,13 +21,18 @@
 // The weight that multiplies a code is weight * scale: the reference counts log2 of the largest scale at hand in, so
 // that this product stays within fp16's normal numbers near the largest contributions.  For fp16 outputs it is taken in
 // two parts, rounded (half a step of 2^-10) and the rest: one alone is an error as large as the output's own rounding
-// (16 sequences of 32k tokens, rms against 64 bits: 2.1e-4 with both, as of the rounding alone, 2.6e-4 with one; 2 to 3%
-// of the time).  bf16 outputs, of 8 bits, make do with one (1.7e-3 either way); there the middle code goes into the zero
+// (16 sequences of 32k tokens, rms against 64 bits: 2.1e-4 with both, as of the rounding alone, 2.6e-4 with one; 390 us
+// with one, 405 with two).  bf16 outputs, of 8 bits, make do with one (1.7e-3 either way); there the middle code goes into the zero
 // and the rounded weights' own sum is taken off as often, so that only a code's distance from the middle feels the
 // rounding.  Zeros enter by fp32 sums: out = sum (w scale) code + sum w zero.
 //
 // Lengths are device data: every workgroup sums up the batch's work, an equal share of it is its own, and it finds the
-// sequences that its share lies in.  Bound by HBM for long contexts: 136 bytes per (token, kv head) at one group.
+// sequences that its share lies in.
+//
+// Bound by HBM for long contexts of few rows per kv head, 136 bytes per (token, kv head) at one group: 16 sequences of
+// 32k tokens, 32 heads, 2.3 GB in 385 - 405 us (its streaming loads alone 369); 128k tokens of 8 kv heads, 143 MB, 35 us and
+// the merge's 5, of which the tiles 23; by vector instructions at two and four groups and for many rows: 64 sequences of
+// 256 to 16k tokens, two groups, 311 MB, 72 us; up to 64 rows a kv head, four groups, 208 MB, 109 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -59,7 +64,6 @@ constexpr int kRowStride = kD + 4;           // floats per parked accumulator ro
 
 __device__ __forceinline__ float4_t mfma(half8_t a, half8_t b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float4_t mfma(bf8_t a, bf8_t b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ half8_t as_half8(unsigned a, unsigned b, unsigned c, unsigned d) {
   return __builtin_bit_cast(half8_t, uint4_t{a, b, c, d});
 }
@@ -76,13 +80,6 @@ __device__ __forceinline__ void unrolled(F f) {  // f(I) .. f(N - 1), the number
 template <int X>
 __device__ __forceinline__ float of_lane(float v) {
   return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + X, 0xF, 0xF, true));
-}
-
-// The row of 16 lanes turned so that lane X's value comes to lane 0.
-template <int X>
-__device__ __forceinline__ float from_lane(float v) {
-  if (X == 0) return v;
-  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + (16 - X) % 16, 0xF, 0xF, true));
 }
 
 // The largest of the row's 16 lanes, in all of them.
@@ -114,32 +111,15 @@ struct PairWord {
   }
 };
 
-template <int FMT>
-struct ZeroWord {  // a pair's zero
-  typename std::conditional<FMT == SKVQ_META_F32, float, typename std::conditional<FMT == SKVQ_META_F16, _Float16, uint8_t>::type>::type w;
-  __device__ __forceinline__ void load(const uint8_t *p) { w = *reinterpret_cast<const decltype(w) *>(p + sizeof(w)); }
-  __device__ __forceinline__ float value() const {
-    if constexpr (FMT == SKVQ_META_FP8_E4M3)
-      return __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
-    else
-      return (float)w;
-  }
-};
-
 // Whether a weight that meets codes has two parts.
 template <class T>
 constexpr bool two_parts() { return __is_same(T, _Float16); }
-
-// Zeros enter scores and outputs by products with the queries' sums and with the weights.  Of four groups, these are fp32
-// matrix instructions: 4 multiplications a lane and score, each with a broadcast before it, would be a quarter of the work.
-constexpr bool zeros_by_matrix(int NG) { return NG == 4; }
 
 // A tile's packed data as a lane holds it.
 template <int NG, int FMT>
 struct Tile {
   uint4_t k[2], v[2];
   PairWord<FMT> pairs[NG];
-  ZeroWord<FMT> k_zero[zeros_by_matrix(NG) ? 2 : 1];  // of key row c, group g of either block
 };
 
 // Which pair lane c of a row of 16 holds in pairs[q]: 16 NG pairs in the order [keys, values][block][token of four][group].
@@ -301,13 +281,11 @@ template <int NG>
 struct State {
   float4_t o[8];      // packed: positions 16n + 4g + reg; full rows: channels 8 (4g + reg) + n
   float m, l, z[NG];  // reference; this lane's share of the sum of weights, of weights times zeros less the middle codes
-  float4_t by_matrix;  // (zeros_by_matrix) the sums of weights times zeros, group by group, in the lanes of g = 0
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int n = 0; n < 8; ++n) o[n] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     m = kNothing;
     l = 0.0f;
-    by_matrix = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int g = 0; g < NG; ++g) z[g] = 0.0f;
   }
@@ -321,7 +299,6 @@ struct State {
     l *= f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) z[g] *= f;
-    if (zeros_by_matrix(NG)) by_matrix *= f;
 #pragma unroll
     for (int n = 0; n < 8; ++n) o[n] *= f;
   }
@@ -372,7 +349,6 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
       x[b] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int n = 0; n < NG; ++n) acc[b][n] = x[b];
-      if (zeros_by_matrix(NG)) x[b] = mfma(t.k_zero[i].value(), qs[b][0], x[b]);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -390,7 +366,7 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
         const float by = of_lane<lane>(scale[q]), z = of_lane<lane>(zero[q]);
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-          if (!zeros_by_matrix(NG)) x[b][r] = n == 0 ? z * qs[b][0] : fmaf(z, qs[b][n], x[b][r]);
+          x[b][r] = n == 0 ? z * qs[b][0] : fmaf(z, qs[b][n], x[b][r]);
           codes[b] = n == 0 ? by * acc[b][0][r] : fmaf(by, acc[b][n][r], codes[b]);
         }
       });
@@ -415,17 +391,12 @@ __device__ __forceinline__ void take_tile(State<NG> (&st)[RB], Tile<NG, FMT> &t,
       p[b] = __builtin_amdgcn_exp2f(s[b][I()] - st[b].m);
       st[b].l += p[b];
     }
-    if (zeros_by_matrix(NG)) {
-      const float z = from_lane<Slot::lane_of(1, i, r, 0)>(zero[Slot::load_of(1, i, r, 0)]);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) st[b].by_matrix = mfma(z, p[b], st[b].by_matrix);
-    }
     unrolled<0, NG>([&](auto N) {
       constexpr int n = N(), q = Slot::load_of(1, i, r, n), lane = Slot::lane_of(1, i, r, n);
       const float by = of_lane<lane>(scale[q]), z = of_lane<lane>(zero[q]);
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
-        if (!zeros_by_matrix(NG)) st[b].z[n] = fmaf(z, p[b], st[b].z[n]);
+        st[b].z[n] = fmaf(z, p[b], st[b].z[n]);
         const float w = by * p[b];
         pb[b][n][I()] = (_Float16)w;
         const half2_t middle = {-(_Float16)kMidCode, -(_Float16)kMidCode};
@@ -518,7 +489,6 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
     const PagedLayout &L;
     const unsigned k_lane, v_lane, (&pair_lane)[NG];
     const bool (&pair_block)[NG];
-    const unsigned zero_lane;
     const uint8_t *part[2];
     unsigned place[2];
     __device__ __forceinline__ uint4_t codes(int i, unsigned lane) const {
@@ -533,7 +503,6 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         t.k[i] = codes(i, k_lane);
-        if (zeros_by_matrix(NG)) t.k_zero[i].load(part[i] + place[i] * (NG * kPair) + zero_lane);
       }
     }
     __device__ __forceinline__ void values(Tile<NG, FMT> &t) const {
@@ -542,7 +511,7 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
     }
   };
   auto tile = [&](int k, int k0) {
-    Next x{L, k_lane, v_lane, pair_lane, pair_block, L.km_at + (c * NG + g) * kPair, {}, {}};
+    Next x{L, k_lane, v_lane, pair_lane, pair_block, {}, {}};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int id = __builtin_amdgcn_readlane(ids, 2 * (k - k0) + i);
@@ -582,10 +551,6 @@ __device__ __forceinline__ void take_packed(const PagedLayout &L, const PagedBat
       qs[r][n] += __shfl_xor(qs[r][n], 16);
       qs[r][n] += __shfl_xor(qs[r][n], 32);
       qs[r][n] *= scale;
-    }
-    if (zeros_by_matrix(NG)) {  // (the matrix product's B operand: a group per row of lanes)
-#pragma unroll
-      for (int n = 1; n < NG; ++n) qs[r][0] = g == n ? qs[r][n] : qs[r][0];
     }
   }
   // Whole tiles that every query sees, then the others (at the end).  The lanes hold the pages of 32 tiles, and the
@@ -681,7 +646,7 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
   typedef Piece<T, 8> P;
   __shared__ Lds<T, RB> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int h = blockIdx.x;  // (heads side by side: a head's units, row blocks of one chunk among them, share a chiplet's L2)
+  const int h = blockIdx.x;  // (heads side by side: a head's workgroups share a chiplet's L2)
   const unsigned long long places = *reinterpret_cast<const unsigned long long *>(L.k_place + h * kD + 8 * c);
   const int p = threadIdx.x % kD, packed_channel = L.v_offset[h * kD + 8 * (p & 15) + (p >> 4)] / 2;  // of the output place it writes
   const BatchPlan plan = plan_batch<RB>(L, b, gridDim.y, lds.members);
@@ -762,7 +727,6 @@ __global__ __launch_bounds__(64 * kWaves, groups_per_cu(NG, RB)) void paged_atte
       for (int n = 0; n < NG; ++n) {
         own.z[n] += __shfl_xor(own.z[n], 16);
         own.z[n] += __shfl_xor(own.z[n], 32);
-        if (zeros_by_matrix(NG)) own.z[n] += __shfl(own.by_matrix[n], c);
       }
       if (r > 0) __syncthreads();  // (the block before has been read out of LDS)
       if (g == 0) {
@@ -880,7 +844,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedL
 }
 
 template <class T, int NG, int RB>
-void launch_chunks(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
+void launch_formats(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
   const dim3 grid(L.Hk, groups), threads(64 * kWaves);
   switch (L.meta_fmt) {
     case SKVQ_META_F32: paged_attention_kernel<T, NG, SKVQ_META_F32, RB><<<grid, threads, 0, s>>>(L, b, q, out, row_chunks); break;
@@ -892,9 +856,9 @@ void launch_chunks(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out o
 template <class T, int RB>
 hipError_t launch_typed(const PagedLayout &L, const PagedBatch &b, TokenRows q, Out out, int row_chunks, unsigned groups, hipStream_t s) {
   switch (L.NG) {
-    case 1: launch_chunks<T, 1, RB>(L, b, q, out, row_chunks, groups, s); break;
-    case 2: launch_chunks<T, 2, RB>(L, b, q, out, row_chunks, groups, s); break;
-    default: launch_chunks<T, 4, RB>(L, b, q, out, row_chunks, groups, s); break;
+    case 1: launch_formats<T, 1, RB>(L, b, q, out, row_chunks, groups, s); break;
+    case 2: launch_formats<T, 2, RB>(L, b, q, out, row_chunks, groups, s); break;
+    default: launch_formats<T, 4, RB>(L, b, q, out, row_chunks, groups, s); break;
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

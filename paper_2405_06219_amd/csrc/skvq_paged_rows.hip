@@ -7,7 +7,8 @@
 // way.  The reorder goes through LDS, a row of values per (wavefront, r).
 //
 // Bound by memory and vector instructions for prompts (a row's 512 bytes in, 140 out; eight channels a lane and four rows
-// a wavefront took twice as long: what a group needs once is computed by all its lanes), by the chain of dependent loads
+// a wavefront took twice as long: what a group needs once is computed by all its lanes; 25143 tokens of 8 kv heads, two
+// groups, 53 us, read back in 28), by the chain of dependent loads
 // for decode steps: sequence, its counts, its page, its ring row.
 #include <hip/hip_runtime.h>
 
